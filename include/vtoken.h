@@ -449,6 +449,132 @@ vtoken_status vtoken_paged_decode_noalloc(const vtoken_cache* cache,
                                           const int32_t* slot_indptr, const int32_t* slots,
                                           hipStream_t stream);
 
+/* ---- Rows of the cache and attention for prompts (what a model does around the passes) ----
+ *
+ * Writing new tokens' K and V into the cache, reading rows back, and attention of a ragged batch
+ * of queries over it. Activations (q, k, v, outputs) are fp16 or bf16 (VTOKEN_KV_FP16 or
+ * VTOKEN_KV_BF16 in `dtype`) with a stride in elements between tokens, the heads of a token side
+ * by side; pointers to them must be aligned to 16 bytes and strides be multiples of 8 elements
+ * (VTOKEN_ERR_ARGUMENT otherwise). An fp16 cache takes fp16 activations, a bf16 or 4-bit cache
+ * bf16, an fp8 cache either.
+ *
+ * 4-bit caches (VTOKEN_KV_MXFP4): a row is the codes [num_kv_heads][head_dim / 2] (e2m1: 0, 0.5,
+ * 1, 1.5, 2, 3, 4, 6 and a sign in bit 3; even values in the low half of a byte), then the
+ * exponents [num_kv_heads][head_dim / 32] (e8m0: value = e2m1 * 2^(e - 127), 255 is NaN), padded
+ * to a multiple of 16 bytes. Such a row is moved as it is by every call that moves rows: describe
+ * the cache to them as num_kv_heads 1, head_dim vtoken_kv_row_bytes(), elem_bytes 1; the calls
+ * below carry the heads and head_dim themselves (for the other types equal to the cache's). */
+enum { VTOKEN_KV_MXFP4 = 3 };
+
+/* Bytes of one token's row in one plane; -1 for sizes that no call takes (head_dim must be a
+ * multiple of 8 up to 256, of 32 for 4-bit caches). */
+int64_t vtoken_kv_row_bytes(int32_t num_kv_heads, int32_t head_dim, int32_t kv_dtype);
+
+/* The append of new tokens (the caller's sync_new_tokens of Sec. 3.2) for one layer: per head of
+ * q and k an RMS norm, then the rotary positions; k and v go to their slots of the cache, q to
+ * q_out (which may be q). For token t at slots[t]:
+ *   y = x * r * w,  r = 1 / sqrt(mean(x^2) + eps), mean and root in 64 bits, r in 32 (no weight:
+ *   y = x);  the first rotary_dim values of y are turned by the position's angles, pairs
+ *   (i, i + rotary_dim / 2), or (2i, 2i + 1) if interleaved: (a, b) -> (a c - b s, b c + a s).
+ * All in float32, rounded once (nearest even): to dtype for q, to the cache's type for k and v.
+ * fp8 saturates at 448; 4 bits take per 32 values the exponent floor(log2(max |y|)) - 2, at least
+ * 2^-126, and saturate at 6 (an infinity or NaN makes the 32 values NaN).
+ * A negative slot marks padding: nothing of that token is read or written. A slot past the pool,
+ * or a position outside [0, num_positions) where there is a table, writes nothing to the cache and
+ * NaN to the token's q_out. Slots of a call must differ (of two tokens with one slot, which values
+ * stay is not defined). */
+typedef struct vtoken_kv_write {
+  const void*  q;            /* device [num_tokens][num_q_heads][head_dim]; NULL if num_q_heads 0  */
+  const void*  k;            /* device [num_tokens][num_kv_heads][head_dim]                        */
+  const void*  v;            /* device, as k                                                       */
+  void*        q_out;        /* device, as q                                                       */
+  int64_t      q_stride, k_stride, v_stride, q_out_stride;  /* elements between tokens             */
+  const float* q_weight;     /* device [head_dim], or NULL: queries are not normalised             */
+  const float* k_weight;     /* device [head_dim], or NULL: keys are not normalised                */
+  const float* cos_sin;      /* device [num_positions][rotary_dim]: cosines, then sines, of each   */
+                             /* position's rotary_dim / 2 angles; NULL: no rotation                */
+  const int32_t* positions;  /* device [num_tokens]; may be NULL without cos_sin                   */
+  const int32_t* slots;      /* device [num_tokens]                                                */
+  int32_t      num_tokens;
+  int32_t      num_q_heads;  /* >= 0                                                               */
+  int32_t      num_kv_heads;
+  int32_t      head_dim;
+  int32_t      rotary_dim;   /* a multiple of 16 (of 8 if interleaved), <= head_dim                */
+  int32_t      num_positions;
+  int32_t      interleaved;  /* 0 or 1                                                             */
+  int32_t      layer;
+  int32_t      dtype;        /* VTOKEN_KV_FP16 or VTOKEN_KV_BF16                                   */
+  int32_t      kv_dtype;     /* VTOKEN_KV_*                                                        */
+  double       eps;
+} vtoken_kv_write;
+
+vtoken_status vtoken_write_kv(const vtoken_cache* cache, const vtoken_kv_write* write,
+                              hipStream_t stream);
+
+/* The K and V rows of listed slots of one layer as dense tensors (a request's cache exported, or
+ * looked at): k_out[i], v_out[i] = values at slots[i], exact in dtype (4-bit values outside bf16's
+ * range aside). A slot outside the pool reads as NaN. Slots may repeat. */
+typedef struct vtoken_kv_read {
+  const int32_t* slots;      /* device [num_tokens]                                                */
+  void*        k_out;        /* device [num_tokens][num_kv_heads][head_dim]                        */
+  void*        v_out;        /* device, as k_out                                                   */
+  int64_t      k_stride, v_stride;   /* elements between tokens                                    */
+  int32_t      num_tokens;
+  int32_t      num_kv_heads;
+  int32_t      head_dim;
+  int32_t      layer;
+  int32_t      dtype;        /* VTOKEN_KV_FP16 or VTOKEN_KV_BF16                                   */
+  int32_t      kv_dtype;     /* VTOKEN_KV_*                                                        */
+} vtoken_kv_read;
+
+vtoken_status vtoken_read_kv(const vtoken_cache* cache, const vtoken_kv_read* read,
+                             hipStream_t stream);
+
+/* Attention of one layer for a ragged batch of queries through a slot mapping (or slot table):
+ * request r has n slots and the queries q_indptr[r] .. q_indptr[r+1], which are its last ones
+ * (their K and V are in the cache). Query i of ql has rank p = n - ql + i among the request's
+ * slots and sees slot k iff
+ *   k <= p  and  (window == 0  or  k > p - window  or  k < sinks),
+ * ranks counted in the mapping's order, over the live tokens only. Query head qh reads KV head
+ * qh / (num_q_heads / num_kv_heads). out = softmax(scale * q . K^T) @ V, sums and softmax in
+ * float32, weights in dtype for the product with V, rounded once to dtype; a query that sees
+ * nothing (ql > n) gives zeros. Rows of q past the last query are neither read nor written.
+ * A query that sees a slot outside the pool gives NaN, no such slot is dereferenced. A request
+ * whose slot range is malformed (negative start or count), which holds more than max_tokens slots
+ * or more than max_queries queries gives NaN for its queries; one whose query range is
+ * not within [0, num_queries] writes nothing. slots may be NULL if no request holds any. A NaN or infinity in K or V reaches the
+ * queries that see it and no other.
+ * The work is split over the slots where few queries meet many of them; the partial sums go to the
+ * workspace, which is overwritten by every call (calls sharing it must be stream-ordered). */
+typedef struct vtoken_attention {
+  const void*  q;            /* device [num_queries][num_q_heads][head_dim]                        */
+  void*        out;          /* device, as q; must not overlap it                                  */
+  int64_t      q_stride, out_stride;   /* elements between queries                                 */
+  const int32_t* q_indptr;   /* device [num_reqs + 1], or NULL: query r is request r's only one    */
+  const int32_t* slot_count; /* device [num_reqs] or NULL, as in vtoken_decode                     */
+  float*       workspace;    /* device, >= vtoken_attention_workspace_bytes() bytes                */
+  int64_t      workspace_bytes;
+  int32_t      num_queries;  /* rows of q and out; >= num_reqs without q_indptr                    */
+  int32_t      max_queries;  /* [host] >= every request's queries; 1 without q_indptr              */
+  int32_t      max_tokens;   /* [host] >= the slot count of every request                          */
+  int32_t      num_q_heads;  /* a multiple of num_kv_heads, at most 16 times as many               */
+  int32_t      num_kv_heads;
+  int32_t      head_dim;     /* 32, 64, 128 or 256                                                 */
+  int32_t      layer;
+  int32_t      dtype;        /* VTOKEN_KV_FP16 or VTOKEN_KV_BF16                                   */
+  int32_t      kv_dtype;     /* VTOKEN_KV_*                                                        */
+  int32_t      window;       /* 0: every earlier token; else >= 1, the query's own token counted   */
+  int32_t      sinks;        /* >= 0: first tokens that stay visible                               */
+  float        scale;        /* softmax scale, usually 1/sqrt(head_dim)                            */
+} vtoken_attention;
+
+/* Bytes of workspace for a call with these sizes (device pointers are not read; 0: none is
+ * needed); -1 for sizes that vtoken_paged_attention refuses. */
+int64_t vtoken_attention_workspace_bytes(const vtoken_attention* attention, int32_t num_reqs);
+vtoken_status vtoken_paged_attention(const vtoken_cache* cache, const vtoken_attention* attention,
+                                     int32_t num_reqs, const int32_t* slot_indptr,
+                                     const int32_t* slots, hipStream_t stream);
+
 /* The hipError_t behind the calling thread's most recent VTOKEN_ERR_HIP (0 if none yet). */
 int32_t vtoken_last_hip_error(void);
 

@@ -74,7 +74,44 @@ class CDecode(ctypes.Structure):
                 ("workspace_bytes", ctypes.c_int64), ("slot_count", ctypes.c_void_p)]
 
 
-KV_FP16, KV_BF16, KV_FP8_E4M3 = 0, 1, 2
+KV_FP16, KV_BF16, KV_FP8_E4M3, KV_MXFP4 = 0, 1, 2, 3
+
+
+class CKVWrite(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q_out", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("q_out_stride", ctypes.c_int64), ("q_weight", ctypes.c_void_p),
+                ("k_weight", ctypes.c_void_p), ("cos_sin", ctypes.c_void_p),
+                ("positions", ctypes.c_void_p), ("slots", ctypes.c_void_p),
+                ("num_tokens", ctypes.c_int32), ("num_q_heads", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("num_positions", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("layer", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("kv_dtype", ctypes.c_int32),
+                ("eps", ctypes.c_double)]
+
+
+class CKVRead(ctypes.Structure):
+    _fields_ = [("slots", ctypes.c_void_p), ("k_out", ctypes.c_void_p),
+                ("v_out", ctypes.c_void_p), ("k_stride", ctypes.c_int64),
+                ("v_stride", ctypes.c_int64), ("num_tokens", ctypes.c_int32),
+                ("num_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("layer", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("kv_dtype", ctypes.c_int32)]
+
+
+class CAttention(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("out", ctypes.c_void_p), ("q_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64), ("q_indptr", ctypes.c_void_p),
+                ("slot_count", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_int64), ("num_queries", ctypes.c_int32),
+                ("max_queries", ctypes.c_int32), ("max_tokens", ctypes.c_int32),
+                ("num_q_heads", ctypes.c_int32), ("num_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("layer", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("kv_dtype", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
 
 
 class CPlannerParams(ctypes.Structure):
@@ -152,6 +189,17 @@ _SIGNATURES = {
                                              ctypes.c_void_p, ctypes.POINTER(CPlannerParams),
                                              ctypes.POINTER(CPlannerState),
                                              ctypes.POINTER(CPlan), ctypes.c_void_p]),
+    "vtoken_kv_row_bytes": (ctypes.c_int64, [ctypes.c_int32, ctypes.c_int32, ctypes.c_int32]),
+    "vtoken_write_kv": (ctypes.c_int32, [ctypes.POINTER(CCache), ctypes.POINTER(CKVWrite),
+                                         ctypes.c_void_p]),
+    "vtoken_read_kv": (ctypes.c_int32, [ctypes.POINTER(CCache), ctypes.POINTER(CKVRead),
+                                        ctypes.c_void_p]),
+    "vtoken_attention_workspace_bytes": (ctypes.c_int64, [ctypes.POINTER(CAttention),
+                                                          ctypes.c_int32]),
+    "vtoken_paged_attention": (ctypes.c_int32, [ctypes.POINTER(CCache),
+                                                ctypes.POINTER(CAttention), ctypes.c_int32,
+                                                ctypes.c_void_p, ctypes.c_void_p,
+                                                ctypes.c_void_p]),
     "vtoken_last_hip_error": (ctypes.c_int32, []),
     "vtoken_status_string": (ctypes.c_char_p, [ctypes.c_int32]),
     "vtoken_version": (ctypes.c_int32, []),
@@ -248,6 +296,35 @@ class KVCache(_Cached):
     def _make_c(self) -> CCache:
         return CCache(_ptr(self.kv), self.num_layers, self.num_kv_heads, self.head_dim,
                       self.block_size, self.num_blocks, self.elem_bytes)
+
+
+class PackedKVCache(KVCache):
+    """A paged KV cache of 4-bit rows (MXFP4): a uint8 tensor [2L][num_blocks][S][row bytes] with
+    the row layout that vtoken.h states. The passes and tables take it like any other cache (its
+    rows move as bytes); write_kv, read_kv and paged_attention deal with its values."""
+
+    def __init__(self, kv, num_layers: int, num_kv_heads: int, head_dim: int, block_size: int):
+        import torch
+        if kv.dtype != torch.uint8:
+            raise ValueError("a 4-bit cache is a uint8 tensor of rows")
+        self.row_bytes = kv_row_bytes(num_kv_heads, head_dim, KV_MXFP4)
+        super().__init__(kv, num_layers, 1, self.row_bytes, block_size)
+        self.num_kv_heads, self.head_dim = int(num_kv_heads), int(head_dim)
+        self.kv_dtype = KV_MXFP4
+
+    @classmethod
+    def allocate(cls, num_layers: int, num_kv_heads: int, head_dim: int, block_size: int,
+                 num_blocks: int, device="cuda"):
+        """A cache of zeros (which stand for zeros)."""
+        import torch
+        row = kv_row_bytes(num_kv_heads, head_dim, KV_MXFP4)
+        kv = torch.zeros(2 * num_layers, num_blocks, block_size, row, dtype=torch.uint8,
+                         device=device)
+        return cls(kv, num_layers, num_kv_heads, head_dim, block_size)
+
+    def _make_c(self) -> CCache:
+        return CCache(_ptr(self.kv), self.num_layers, 1, self.row_bytes, self.block_size,
+                      self.num_blocks, 1)
 
 
 class Batch(_Cached):
@@ -630,3 +707,211 @@ def run_partial_pass(cache: KVCache, batch: Batch, slot_in, plan: Optional[Plan]
     plan_partial(cache, batch, slot_in, plan, state, params, stream)
     repack(cache, batch, plan, stream)
     return plan, state
+
+
+def kv_row_bytes(num_kv_heads: int, head_dim: int, kv_dtype: int) -> int:
+    n = load_library().vtoken_kv_row_bytes(int(num_kv_heads), int(head_dim), int(kv_dtype))
+    if n < 0:
+        raise VTokenError(STATUS_CODE["VTOKEN_ERR_SHAPE"], "vtoken_kv_row_bytes")
+    return n
+
+
+def rotary_table(num_positions: int, rotary_dim: int, base: float = 10000.0, device="cuda"):
+    """cos_sin of write_kv: float32 [num_positions][rotary_dim], the cosines of position p's
+    angles p * base^(-2i / rotary_dim), then their sines (angles in float64: in float32 those of
+    far positions are off by several degrees)."""
+    import torch
+    half = int(rotary_dim) // 2
+    i = torch.arange(half, dtype=torch.float64, device=device)
+    p = torch.arange(int(num_positions), dtype=torch.float64, device=device)
+    angle = p[:, None] * float(base) ** (-i / half)
+    return torch.cat([angle.cos(), angle.sin()], 1).float()
+
+
+def _activation(x, name: str, device, dtype, heads: int, head_dim: int) -> int:
+    """A [tokens][heads][head_dim] activation tensor's stride between tokens, in elements."""
+    if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != head_dim:
+        raise ValueError(f"{name} must be [tokens][{heads}][{head_dim}]")
+    if x.dtype != dtype or x.device != device:
+        raise ValueError(f"{name} must be {dtype} on {device}")
+    if (heads > 1 and x.stride(1) != head_dim) or x.stride(2) != 1:
+        raise ValueError(f"the heads of a token must be contiguous in {name}")
+    return x.stride(0) if x.shape[0] > 1 else heads * head_dim
+
+
+def _ints(x, name: str, device, numel: Optional[int] = None) -> None:
+    import torch
+    if x.dtype != torch.int32 or x.device != device or not x.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous int32 tensor on {device}")
+    if numel is not None and x.numel() < numel:
+        raise ValueError(f"{name} must have {numel} entries")
+
+
+def _act_code(dtype) -> int:
+    import torch
+    if dtype == torch.bfloat16:
+        return KV_BF16
+    if dtype == torch.float16:
+        return KV_FP16
+    raise ValueError(f"activations are fp16 or bf16, not {dtype}")
+
+
+def _cache_code(cache: KVCache, kv_dtype) -> int:
+    if kv_dtype is not None:
+        return int(kv_dtype)
+    code = getattr(cache, "kv_dtype", None)
+    return kv_dtype_code(cache.kv.dtype) if code is None else code
+
+
+def _on_device(device, stream, call):
+    """call(stream) with the tensors' device current, on `stream` or that device's current one."""
+    import torch
+    if device.index is None or device.index == torch.cuda.current_device():
+        return call(_stream(stream))
+    with torch.cuda.device(device):
+        return call(_stream(stream))
+
+
+def write_kv(cache: KVCache, k, v, slots, layer: int, q=None, positions=None, cos_sin=None,
+             q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False,
+             q_out=None, kv_dtype=None, stream=None):
+    """New tokens of one layer into the cache: per-head RMS norm of q and k (where there are
+    weights, float32 [head_dim]), rotary positions (where there is a table, rotary_table), k and v
+    stored at `slots` (int32; negative: padding, left alone) in the cache's type. q, k, v are fp16
+    or bf16 [tokens][heads][head_dim], the tokens at any stride (views of a fused projection).
+    Returns q_out (q may be given for it), or None without q; rows of padding tokens in a q_out
+    made here are not set."""
+    import torch
+    lib = load_library()
+    dev = cache.kv.device
+    H, D, n = cache.num_kv_heads, cache.head_dim, int(slots.numel())
+    _ints(slots, "slots", dev)
+    w = CKVWrite(num_tokens=n, num_kv_heads=H, head_dim=D, layer=int(layer), eps=float(eps),
+                 interleaved=int(bool(interleaved)), dtype=_act_code(k.dtype),
+                 kv_dtype=_cache_code(cache, kv_dtype), slots=_ptr(slots), k=_ptr(k), v=_ptr(v),
+                 k_stride=_activation(k, "k", dev, k.dtype, H, D),
+                 v_stride=_activation(v, "v", dev, k.dtype, H, D))
+    if k.shape[0] < n or v.shape[0] < n:
+        raise ValueError("k and v must have a row for every slot")
+    if q is not None:
+        heads = int(q.shape[1]) if q.dim() == 3 else 0
+        w.num_q_heads, w.q = heads, _ptr(q)
+        w.q_stride = _activation(q, "q", dev, k.dtype, heads, D)
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        w.q_out, w.q_out_stride = _ptr(q_out), _activation(q_out, "q_out", dev, k.dtype, heads, D)
+        if q.shape[0] < n or q_out.shape[0] < n:
+            raise ValueError("q and q_out must have a row for every slot")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    for name, x in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if x is not None:
+            if x.dtype != torch.float32 or x.device != dev or x.shape != (D,) or \
+                    not x.is_contiguous():
+                raise ValueError(f"{name} must be float32 [{D}] on {dev}")
+            setattr(w, name, _ptr(x))
+    if cos_sin is not None:
+        if positions is None:
+            raise ValueError("a table needs positions")
+        if cos_sin.dtype != torch.float32 or cos_sin.device != dev or cos_sin.dim() != 2 or \
+                not cos_sin.is_contiguous():
+            raise ValueError(f"cos_sin must be contiguous float32 [positions][rotary_dim] on {dev}")
+        _ints(positions, "positions", dev, n)
+        w.cos_sin, w.positions = _ptr(cos_sin), _ptr(positions)
+        w.num_positions, w.rotary_dim = int(cos_sin.shape[0]), int(cos_sin.shape[1])
+    c = cache.c()
+    _check(_on_device(dev, stream, lambda st: lib.vtoken_write_kv(
+        ctypes.byref(c), ctypes.byref(w), st)), "vtoken_write_kv")
+    return q_out
+
+
+def read_kv(cache: KVCache, slots, layer: int, dtype=None, k_out=None, v_out=None, kv_dtype=None,
+            stream=None):
+    """The rows of listed slots (int32; one outside the pool reads as NaN) of one layer as dense
+    [n][num_kv_heads][head_dim] tensors (k, v), fp16 or bf16 (`dtype`; by default the cache's own
+    type, bf16 for fp8 and 4-bit caches)."""
+    import torch
+    lib = load_library()
+    dev = cache.kv.device
+    H, D, n = cache.num_kv_heads, cache.head_dim, int(slots.numel())
+    _ints(slots, "slots", dev)
+    code = _cache_code(cache, kv_dtype)
+    if dtype is None:
+        dtype = k_out.dtype if k_out is not None else \
+            torch.float16 if code == KV_FP16 else torch.bfloat16
+    if k_out is None:
+        k_out = torch.empty(n, H, D, dtype=dtype, device=dev)
+    if v_out is None:
+        v_out = torch.empty(n, H, D, dtype=dtype, device=dev)
+    r = CKVRead(slots=_ptr(slots), k_out=_ptr(k_out), v_out=_ptr(v_out),
+                k_stride=_activation(k_out, "k_out", dev, dtype, H, D),
+                v_stride=_activation(v_out, "v_out", dev, dtype, H, D), num_tokens=n,
+                num_kv_heads=H, head_dim=D, layer=int(layer), dtype=_act_code(dtype),
+                kv_dtype=code)
+    if k_out.shape[0] < n or v_out.shape[0] < n:
+        raise ValueError("k_out and v_out must have a row for every slot")
+    c = cache.c()
+    _check(_on_device(dev, stream, lambda st: lib.vtoken_read_kv(
+        ctypes.byref(c), ctypes.byref(r), st)), "vtoken_read_kv")
+    return k_out, v_out
+
+
+def attention_workspace_bytes(attention: CAttention, num_reqs: int) -> int:
+    n = load_library().vtoken_attention_workspace_bytes(ctypes.byref(attention), int(num_reqs))
+    if n < 0:
+        raise VTokenError(STATUS_CODE["VTOKEN_ERR_SHAPE"], "vtoken_attention_workspace_bytes")
+    return n
+
+
+def paged_attention(cache: KVCache, q, slot_indptr, slots, layer: int, max_tokens: int,
+                    q_indptr=None, max_queries: Optional[int] = None, window: int = 0,
+                    sinks: int = 0, scale: Optional[float] = None, out=None, workspace=None,
+                    kv_dtype=None, stream=None, slot_count=None):
+    """Causal attention of one layer for a ragged batch of queries through a slot mapping (or,
+    with slot_count, a slot table): request r's queries are q[q_indptr[r] : q_indptr[r+1]] (one
+    each without q_indptr), its last ones. window > 0: a query sees its last `window` tokens, its
+    own counted, and the first `sinks`. q and out are fp16 or bf16 [queries][heads][head_dim].
+    max_tokens and max_queries bound every request's slots and queries (max_queries: by default
+    the number of rows of q). Rows of q past the last query are left alone."""
+    import torch
+    lib = load_library()
+    dev = cache.kv.device
+    D = cache.head_dim
+    heads = int(q.shape[1]) if q.dim() == 3 else 0
+    _ints(slot_indptr, "slot_indptr", dev, 1)
+    _ints(slots, "slots", dev)
+    R = int(slot_indptr.numel()) - 1
+    stride = _activation(q, "q", dev, q.dtype, heads, D)
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    if out.shape != q.shape:
+        raise ValueError("out must match q")
+    if q_indptr is not None:
+        _ints(q_indptr, "q_indptr", dev, R + 1)
+    if slot_count is not None:
+        _ints(slot_count, "slot_count", dev, R)
+    if max_queries is None:
+        max_queries = 1 if q_indptr is None else int(q.shape[0])
+    a = CAttention(
+        q=_ptr(q), out=_ptr(out), q_stride=stride,
+        out_stride=_activation(out, "out", dev, q.dtype, heads, D), q_indptr=_ptr(q_indptr),
+        slot_count=_ptr(slot_count), num_queries=int(q.shape[0]), max_queries=int(max_queries),
+        max_tokens=int(max_tokens), num_q_heads=heads, num_kv_heads=cache.num_kv_heads,
+        head_dim=D, layer=int(layer), dtype=_act_code(q.dtype),
+        kv_dtype=_cache_code(cache, kv_dtype), window=int(window), sinks=int(sinks),
+        scale=float(D ** -0.5 if scale is None else scale))
+    need = attention_workspace_bytes(a, R)
+    if workspace is None and need > 0:
+        workspace = torch.empty((need + 3) // 4, dtype=torch.float32, device=dev)
+        if stream is not None and hasattr(stream, "cuda_stream"):
+            workspace.record_stream(stream)
+    if workspace is not None:
+        if workspace.device != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace must be contiguous on {dev}")
+        a.workspace = _ptr(workspace)
+        a.workspace_bytes = int(workspace.numel() * workspace.element_size())
+    c = cache.c()
+    _check(_on_device(dev, stream, lambda st: lib.vtoken_paged_attention(
+        ctypes.byref(c), ctypes.byref(a), R, _ptr(slot_indptr), _ptr(slots), st)),
+        "vtoken_paged_attention")
+    return out

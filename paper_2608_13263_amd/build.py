@@ -21,7 +21,8 @@ LIB_PATH = os.path.join(HERE, "libvtoken.so")
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = [os.path.join(CSRC, f)
            for f in ("vtoken_abi.hip", "vtoken_kernels.hip", "vtoken_copy.hip",
-                     "vtoken_attention.hip", "vtoken_planner.hip", "vtoken_layout.hip")]
+                     "vtoken_attention.hip", "vtoken_planner.hip", "vtoken_layout.hip",
+                     "vtoken_rows.hip", "vtoken_prompt.hip")]
 HEADERS = [os.path.join(ROOT, "include", "vtoken.h"), os.path.join(CSRC, "vtoken_internal.h")]
 ARCH = "gfx950"
 

@@ -582,6 +582,245 @@ vtoken_status vtoken_plan_partial(const vtoken_cache* cache, const vtoken_batch*
   return hip_status(vtoken::launch_planner(a, stream));
 }
 
+int64_t vtoken_kv_row_bytes(int32_t num_kv_heads, int32_t head_dim, int32_t kv_dtype) {
+  if (num_kv_heads <= 0 || head_dim <= 0 || head_dim % 8 != 0 || head_dim > 256) return -1;
+  const int64_t values = (int64_t)num_kv_heads * head_dim;
+  switch (kv_dtype) {
+    case VTOKEN_KV_FP16:
+    case VTOKEN_KV_BF16: return 2 * values;
+    case VTOKEN_KV_FP8_E4M3: return values;
+    case VTOKEN_KV_MXFP4:
+      return head_dim % 32 != 0 ? -1 : (values / 2 + values / 32 + 15) / 16 * 16;
+    default: return -1;
+  }
+}
+
+}  // extern "C"
+
+namespace {
+
+// The heads, types and layer of a call that reads or writes rows as values.
+vtoken_status check_rows(const vtoken_cache* c, int32_t heads, int32_t head_dim, int32_t layer,
+                         int32_t dtype, int32_t kv_dtype) {
+  const int64_t row = vtoken_kv_row_bytes(heads, head_dim, kv_dtype);
+  if (row < 0 || layer < 0 || layer >= c->num_layers) return VTOKEN_ERR_SHAPE;
+  const int bytes = kv_dtype == VTOKEN_KV_FP16 || kv_dtype == VTOKEN_KV_BF16 ? 2 : 1;
+  if (c->elem_bytes != bytes || (int64_t)c->num_kv_heads * c->head_dim * bytes != row) {
+    return VTOKEN_ERR_SHAPE;
+  }
+  if (kv_dtype != VTOKEN_KV_MXFP4 && (c->num_kv_heads != heads || c->head_dim != head_dim)) {
+    return VTOKEN_ERR_SHAPE;
+  }
+  if (dtype != VTOKEN_KV_FP16 && dtype != VTOKEN_KV_BF16) return VTOKEN_ERR_SHAPE;
+  if (kv_dtype == VTOKEN_KV_MXFP4 ? dtype != VTOKEN_KV_BF16
+                                  : kv_dtype != VTOKEN_KV_FP8_E4M3 && dtype != kv_dtype) {
+    return VTOKEN_ERR_SHAPE;
+  }
+  return VTOKEN_OK;
+}
+
+// An activation tensor: 16-byte aligned rows of `width` elements that do not overlap.
+vtoken_status check_activation(const void* p, int64_t stride, int64_t width, int32_t tokens) {
+  if (p == nullptr) return VTOKEN_ERR_NULL;
+  if (reinterpret_cast<uintptr_t>(p) % 16 != 0 || stride % 8 != 0 ||
+      (tokens > 1 && stride < width)) {
+    return VTOKEN_ERR_ARGUMENT;
+  }
+  return VTOKEN_OK;
+}
+
+int64_t plane_bytes_of(const vtoken_cache* c) {
+  return (int64_t)c->num_blocks * c->block_size * c->num_kv_heads * c->head_dim * c->elem_bytes;
+}
+
+}  // namespace
+
+extern "C" {
+
+vtoken_status vtoken_write_kv(const vtoken_cache* cache, const vtoken_kv_write* w,
+                              hipStream_t stream) {
+  vtoken_status s = check_cache(cache);
+  if (s != VTOKEN_OK) return s;
+  if (w == nullptr) return VTOKEN_ERR_NULL;
+  if ((s = check_rows(cache, w->num_kv_heads, w->head_dim, w->layer, w->dtype, w->kv_dtype)) !=
+      VTOKEN_OK) {
+    return s;
+  }
+  const int D = w->head_dim;
+  if (w->num_tokens < 0 || w->num_q_heads < 0) return VTOKEN_ERR_SHAPE;
+  if (w->interleaved != 0 && w->interleaved != 1) return VTOKEN_ERR_ARGUMENT;
+  if (w->cos_sin != nullptr &&
+      (w->rotary_dim <= 0 || w->rotary_dim > D || w->num_positions < 0 ||
+       w->rotary_dim % (w->interleaved != 0 ? 8 : 16) != 0)) {
+    return VTOKEN_ERR_SHAPE;
+  }
+  // a work item is a head row of a token; their number fits an int
+  const int64_t items =
+      w->num_tokens * ((int64_t)w->num_q_heads + 2 * (int64_t)w->num_kv_heads);
+  if (items > INT32_MAX) return VTOKEN_ERR_SHAPE;
+  if (w->num_tokens == 0) return VTOKEN_OK;
+  if (w->slots == nullptr || (w->cos_sin != nullptr && w->positions == nullptr)) {
+    return VTOKEN_ERR_NULL;
+  }
+  const int64_t kv_width = (int64_t)w->num_kv_heads * D, q_width = (int64_t)w->num_q_heads * D;
+  if ((s = check_activation(w->k, w->k_stride, kv_width, w->num_tokens)) != VTOKEN_OK) return s;
+  if ((s = check_activation(w->v, w->v_stride, kv_width, w->num_tokens)) != VTOKEN_OK) return s;
+  if (w->num_q_heads > 0) {
+    if ((s = check_activation(w->q, w->q_stride, q_width, w->num_tokens)) != VTOKEN_OK) return s;
+    if ((s = check_activation(w->q_out, w->q_out_stride, q_width, w->num_tokens)) != VTOKEN_OK) {
+      return s;
+    }
+  }
+  vtoken::WriteArgs a = {};
+  a.q = static_cast<const uint8_t*>(w->q);
+  a.k = static_cast<const uint8_t*>(w->k);
+  a.v = static_cast<const uint8_t*>(w->v);
+  a.q_out = static_cast<uint8_t*>(w->q_out);
+  a.q_stride = w->q_stride;
+  a.k_stride = w->k_stride;
+  a.v_stride = w->v_stride;
+  a.q_out_stride = w->q_out_stride;
+  a.q_weight = w->q_weight;
+  a.k_weight = w->k_weight;
+  a.cos_sin = w->cos_sin;
+  a.positions = w->positions;
+  a.slots = w->slots;
+  a.row_bytes = vtoken_kv_row_bytes(w->num_kv_heads, D, w->kv_dtype);
+  a.kplane = static_cast<uint8_t*>(cache->kv) + 2 * (int64_t)w->layer * plane_bytes_of(cache);
+  a.vplane = a.kplane + plane_bytes_of(cache);
+  a.num_tokens = w->num_tokens;
+  a.num_q_heads = w->num_q_heads;
+  a.num_kv_heads = w->num_kv_heads;
+  a.head_dim = D;
+  a.rotary_dim = w->cos_sin != nullptr ? w->rotary_dim : 0;
+  a.num_positions = w->num_positions;
+  a.interleaved = w->interleaved;
+  a.num_slots = cache->num_blocks * cache->block_size;
+  a.eps = w->eps;
+  return hip_status(
+      vtoken::launch_write_kv(a, w->dtype == VTOKEN_KV_BF16, w->kv_dtype, stream));
+}
+
+vtoken_status vtoken_read_kv(const vtoken_cache* cache, const vtoken_kv_read* r,
+                             hipStream_t stream) {
+  vtoken_status s = check_cache(cache);
+  if (s != VTOKEN_OK) return s;
+  if (r == nullptr) return VTOKEN_ERR_NULL;
+  if ((s = check_rows(cache, r->num_kv_heads, r->head_dim, r->layer, r->dtype, r->kv_dtype)) !=
+      VTOKEN_OK) {
+    return s;
+  }
+  if (r->num_tokens < 0 || 2 * (int64_t)r->num_kv_heads * r->num_tokens > INT32_MAX) {
+    return VTOKEN_ERR_SHAPE;
+  }
+  if (r->num_tokens == 0) return VTOKEN_OK;
+  if (r->slots == nullptr) return VTOKEN_ERR_NULL;
+  const int64_t width = (int64_t)r->num_kv_heads * r->head_dim;
+  if ((s = check_activation(r->k_out, r->k_stride, width, r->num_tokens)) != VTOKEN_OK) return s;
+  if ((s = check_activation(r->v_out, r->v_stride, width, r->num_tokens)) != VTOKEN_OK) return s;
+  vtoken::ReadArgs a = {};
+  a.slots = r->slots;
+  a.k_out = static_cast<uint8_t*>(r->k_out);
+  a.v_out = static_cast<uint8_t*>(r->v_out);
+  a.k_stride = r->k_stride;
+  a.v_stride = r->v_stride;
+  a.kplane = static_cast<const uint8_t*>(cache->kv) + 2 * (int64_t)r->layer * plane_bytes_of(cache);
+  a.vplane = a.kplane + plane_bytes_of(cache);
+  a.row_bytes = vtoken_kv_row_bytes(r->num_kv_heads, r->head_dim, r->kv_dtype);
+  a.num_tokens = r->num_tokens;
+  a.num_kv_heads = r->num_kv_heads;
+  a.head_dim = r->head_dim;
+  a.num_slots = cache->num_blocks * cache->block_size;
+  return hip_status(
+      vtoken::launch_read_kv(a, r->dtype == VTOKEN_KV_BF16, r->kv_dtype, stream));
+}
+
+}  // extern "C"
+
+namespace {
+
+// The sizes of an attention call; fills what the launch and the workspace go by.
+vtoken_status attention_sizes(const vtoken_attention* t, int32_t num_reqs,
+                              vtoken::PromptArgs* a) {
+  if (num_reqs < 0 || t->num_queries < 0 || t->max_queries < 0 || t->max_tokens < 0) {
+    return VTOKEN_ERR_SHAPE;
+  }
+  if (t->num_kv_heads <= 0 || t->num_q_heads <= 0 || t->num_q_heads % t->num_kv_heads != 0 ||
+      t->num_q_heads / t->num_kv_heads > 16) {
+    return VTOKEN_ERR_SHAPE;
+  }
+  const int D = t->head_dim;
+  if (D != 32 && D != 64 && D != 128 && D != 256) return VTOKEN_ERR_SHAPE;
+  if (t->kv_dtype < 0 || t->kv_dtype > VTOKEN_KV_MXFP4) return VTOKEN_ERR_SHAPE;
+  if (t->window < 0 || t->sinks < 0) return VTOKEN_ERR_ARGUMENT;
+  if (t->q_indptr == nullptr && (t->max_queries != 1 || t->num_queries < num_reqs)) {
+    return VTOKEN_ERR_SHAPE;
+  }
+  *a = {};
+  a->num_reqs = num_reqs;
+  a->num_queries = t->num_queries;
+  a->max_queries = t->max_queries;
+  a->max_tokens = t->max_tokens;
+  a->num_kv_heads = t->num_kv_heads;
+  a->group = t->num_q_heads / t->num_kv_heads;
+  a->head_dim = D;
+  a->layer = t->layer;
+  a->window = t->window;
+  a->sinks = t->sinks;
+  a->scale = t->scale;
+  return VTOKEN_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t vtoken_attention_workspace_bytes(const vtoken_attention* t, int32_t num_reqs) {
+  vtoken::PromptArgs a;
+  if (t == nullptr || attention_sizes(t, num_reqs, &a) != VTOKEN_OK) return -1;
+  return vtoken::prompt_workspace_bytes(a, t->kv_dtype);
+}
+
+vtoken_status vtoken_paged_attention(const vtoken_cache* cache, const vtoken_attention* t,
+                                     int32_t num_reqs, const int32_t* slot_indptr,
+                                     const int32_t* slots, hipStream_t stream) {
+  vtoken_status s = check_cache(cache);
+  if (s != VTOKEN_OK) return s;
+  if (t == nullptr) return VTOKEN_ERR_NULL;
+  vtoken::PromptArgs a;
+  if ((s = attention_sizes(t, num_reqs, &a)) != VTOKEN_OK) return s;
+  if ((s = check_rows(cache, t->num_kv_heads, t->head_dim, t->layer, t->dtype, t->kv_dtype)) !=
+      VTOKEN_OK) {
+    return s;
+  }
+  if (num_reqs == 0 || t->num_queries == 0) return VTOKEN_OK;
+  if (t->max_queries == 0) return VTOKEN_ERR_SHAPE;
+  if (slot_indptr == nullptr) return VTOKEN_ERR_NULL;
+  if (slots == nullptr) a.max_tokens = 0;   // no request may hold any
+  const int64_t width = (int64_t)t->num_q_heads * t->head_dim;
+  if ((s = check_activation(t->q, t->q_stride, width, t->num_queries)) != VTOKEN_OK) return s;
+  if ((s = check_activation(t->out, t->out_stride, width, t->num_queries)) != VTOKEN_OK) return s;
+  const int64_t need = vtoken_attention_workspace_bytes(t, num_reqs);
+  if (need < 0) return VTOKEN_ERR_SHAPE;
+  if (need > 0 && t->workspace == nullptr) return VTOKEN_ERR_NULL;
+  if (need > t->workspace_bytes) return VTOKEN_ERR_CAPACITY;
+  a.kv = static_cast<const uint8_t*>(cache->kv);
+  a.plane_bytes = plane_bytes_of(cache);
+  a.row_bytes = vtoken_kv_row_bytes(t->num_kv_heads, t->head_dim, t->kv_dtype);
+  a.q = static_cast<const uint8_t*>(t->q);
+  a.out = static_cast<uint8_t*>(t->out);
+  a.q_stride = t->q_stride;
+  a.out_stride = t->out_stride;
+  a.q_indptr = t->q_indptr;
+  a.slot_indptr = slot_indptr;
+  a.slots = slots;
+  a.slot_count = t->slot_count;
+  a.workspace = t->workspace;
+  a.num_slots = cache->num_blocks * cache->block_size;
+  return hip_status(
+      vtoken::launch_prompt(a, t->dtype == VTOKEN_KV_BF16, t->kv_dtype, stream));
+}
+
 int64_t vtoken_check_layout_workspace_bytes(int32_t num_blocks) {
   if (num_blocks <= 0) return -1;
   return 4 * vtoken::layout_words(num_blocks);

@@ -1,0 +1,76 @@
+// Elements of the cache's and the activations' types, shared by the kernels that deal with values
+// (vtoken_rows.hip, vtoken_prompt.hip). Not installed.
+#pragma once
+
+#include <type_traits>
+
+#include "vtoken_internal.h"
+
+namespace vtoken {
+namespace elements {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+// the same in a caller's float buffers, which are aligned to a float and no more
+typedef f32x2 f32x2_in __attribute__((aligned(4)));
+typedef f32x4 f32x4_in __attribute__((aligned(4)));
+
+// The 16-bit type of activations and of matrix-core operands.
+template <bool kBf16>
+struct Act {
+  typedef _Float16 elem;
+  typedef f16x8 x8;
+  typedef f16x2 x2;
+};
+template <>
+struct Act<true> {
+  typedef __bf16 elem;
+  typedef bf16x8 x8;
+  typedef bf16x2 x2;
+};
+
+// e8m0 exponent -> 2^(e - 127) (255: NaN, 0: zero, which no stored row has).
+__device__ __forceinline__ float e8m0_scale(uint32_t e) {
+  return e == 255 ? __builtin_nanf("") : __uint_as_float(e << 23);
+}
+
+// Eight consecutive elements of a cache row as activations: 16 bytes of fp16 / bf16 as they are,
+// 8 bytes of fp8 or 4 bytes of codes through the conversion instructions. Every value is exact
+// (e4m3 in fp16 and bf16, e2m1 times a power of two in bf16).
+template <bool kBf16>
+__device__ __forceinline__ u32x4 widen_fp8(u32x2 w) {
+  u32x4 o;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if constexpr (kBf16) {
+      o[2 * i] = __builtin_bit_cast(
+          uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(w[i]), 1.f, false));
+      o[2 * i + 1] = __builtin_bit_cast(
+          uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(static_cast<int>(w[i]), 1.f, true));
+    } else {
+      o[2 * i] = __builtin_bit_cast(
+          uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(w[i]), 1.f, false));
+      o[2 * i + 1] = __builtin_bit_cast(
+          uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(static_cast<int>(w[i]), 1.f, true));
+    }
+  }
+  return o;
+}
+
+__device__ __forceinline__ u32x4 widen_fp4(uint32_t w, float scale) {
+  u32x4 o;
+  o.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0));
+  o.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1));
+  o.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
+  o.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
+  return o;
+}
+
+}  // namespace elements
+}  // namespace vtoken

@@ -1,5 +1,5 @@
 // Internal declarations shared by the kernels (vtoken_kernels.hip, vtoken_copy.hip,
-// vtoken_attention.hip, vtoken_planner.hip, vtoken_layout.hip) and the C ABI front end
+// vtoken_attention.hip, vtoken_planner.hip, vtoken_layout.hip, vtoken_rows.hip, vtoken_prompt.hip) and the C ABI front end
 // (vtoken_abi.hip). Not installed; the public interface is include/vtoken.h.
 #pragma once
 
@@ -377,6 +377,77 @@ __host__ __device__ constexpr int decode_grid_splits(int splits) { return splits
 // (request, split) pairs of the split launch's grid: whole octets, for the kernels that place the
 // heads of a split on one XCD.
 __host__ __device__ constexpr int64_t decode_grid_groups(int64_t n) { return (n + 7) / 8 * 8; }
+
+// Rows of the cache (vtoken_rows.hip).
+struct WriteArgs {
+  const uint8_t* q;         // activations: 2 bytes per element
+  const uint8_t* k;
+  const uint8_t* v;
+  uint8_t* q_out;
+  int64_t q_stride, k_stride, v_stride, q_out_stride;   // elements
+  const float* q_weight;
+  const float* k_weight;
+  const float* cos_sin;
+  const int32_t* positions;
+  const int32_t* slots;
+  uint8_t* kplane;
+  uint8_t* vplane;
+  int64_t row_bytes;
+  int32_t num_tokens;
+  int32_t num_q_heads;
+  int32_t num_kv_heads;
+  int32_t head_dim;
+  int32_t rotary_dim;
+  int32_t num_positions;
+  int32_t interleaved;
+  int32_t num_slots;
+  double eps;
+};
+struct ReadArgs {
+  const int32_t* slots;
+  uint8_t* k_out;
+  uint8_t* v_out;
+  int64_t k_stride, v_stride;   // elements
+  const uint8_t* kplane;
+  const uint8_t* vplane;
+  int64_t row_bytes;
+  int32_t num_tokens;
+  int32_t num_kv_heads;
+  int32_t head_dim;
+  int32_t num_slots;
+};
+// bf16: the activations' type (else fp16); kind: the cache's VTOKEN_KV_*
+hipError_t launch_write_kv(const WriteArgs& a, bool bf16, int kind, hipStream_t stream);
+hipError_t launch_read_kv(const ReadArgs& a, bool bf16, int kind, hipStream_t stream);
+
+// Attention of a ragged batch of queries (vtoken_prompt.hip).
+struct PromptArgs {
+  const uint8_t* kv;
+  int64_t plane_bytes;
+  int64_t row_bytes;
+  const uint8_t* q;
+  uint8_t* out;
+  int64_t q_stride, out_stride;   // elements
+  const int32_t* q_indptr;        // null: one query per request
+  const int32_t* slot_indptr;
+  const int32_t* slots;
+  const int32_t* slot_count;      // null: counts from slot_indptr
+  float* workspace;
+  int32_t num_reqs;
+  int32_t num_queries;
+  int32_t max_queries;
+  int32_t max_tokens;
+  int32_t num_kv_heads;
+  int32_t group;                  // query heads per KV head
+  int32_t head_dim;
+  int32_t layer;
+  int32_t num_slots;
+  int32_t window;
+  int32_t sinks;
+  float scale;
+};
+int64_t prompt_workspace_bytes(const PromptArgs& a, int kind);
+hipError_t launch_prompt(const PromptArgs& a, bool bf16, int kind, hipStream_t stream);
 
 hipError_t launch_build(const MetaArgs& a, hipStream_t stream);
 // variant: 0 default (4), 1 LDS double buffer, 2 LDS single buffer, 3 registers, 4 row walk
