@@ -757,6 +757,7 @@ vtoken_status attention_sizes(const vtoken_attention* t, int32_t num_reqs,
     return VTOKEN_ERR_SHAPE;
   }
   *a = {};
+  a->q_indptr = t->q_indptr;
   a->num_reqs = num_reqs;
   a->num_queries = t->num_queries;
   a->max_queries = t->max_queries;
@@ -811,7 +812,6 @@ vtoken_status vtoken_paged_attention(const vtoken_cache* cache, const vtoken_att
   a.out = static_cast<uint8_t*>(t->out);
   a.q_stride = t->q_stride;
   a.out_stride = t->out_stride;
-  a.q_indptr = t->q_indptr;
   a.slot_indptr = slot_indptr;
   a.slots = slots;
   a.slot_count = t->slot_count;

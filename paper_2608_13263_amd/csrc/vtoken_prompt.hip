@@ -1,7 +1,12 @@
 // Attention of a ragged batch of queries over the paged cache (vtoken_paged_attention): causal,
 // with a sliding window and first tokens that stay visible, through a slot mapping.
 //
-//   simple_kernel   one wave per (query, query head): 64 keys at a time, running softmax
+//   prompt_kernel    one workgroup per (tile of query rows, KV head, split): both products on the
+//                    matrix cores, a running softmax over 64 keys at a time
+//   combine_kernel   merges the splits (no launch where there is one)
+//
+// A tile's rows are its tokens times the query heads of the KV head, so that one pass over K and V
+// serves them all.
 #include <math.h>
 
 #include "vtoken_elements.h"
@@ -11,114 +16,531 @@ namespace {
 
 using namespace elements;
 
-// One element of head h's row as a float.
-template <int kKind>
-__device__ __forceinline__ float element(const uint8_t* row, int heads, int head_dim, int h,
-                                         int d) {
-  if constexpr (kKind == 0) {
-    return static_cast<float>(reinterpret_cast<const _Float16*>(row)[h * head_dim + d]);
-  } else if constexpr (kKind == 1) {
-    return static_cast<float>(reinterpret_cast<const __bf16*>(row)[h * head_dim + d]);
-  } else if constexpr (kKind == 2) {
-    return __builtin_amdgcn_cvt_f32_fp8(row[h * head_dim + d], 0);
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kWaves = 4;
+constexpr int kThreads = 64 * kWaves;
+constexpr int kRows = 32 * kWaves;   // query rows of a tile: (token, query head of the KV head)
+
+// Keys of a step; with 512-byte head rows half as many (registers of the loads in flight, LDS).
+constexpr int key_tile(int head_dim) { return head_dim > 128 ? 32 : 64; }
+
+constexpr int kMaxSplits = 64;
+
+// Tokens of a tile.
+__host__ __device__ constexpr int tile_tokens(int group) { return kRows / group; }
+
+// A request's part of a call.
+struct Request {
+  int r;        // -1: no tile of any request
+  int q0, ql;   // its queries
+  int tile;     // tile of the request
+};
+
+// The request that holds tile `tau` of the batch, requests' tiles one after the other. Every lane
+// gets the answer; 64 requests at a time.
+__device__ __forceinline__ Request find_request(const PromptArgs& a, int tau) {
+  Request f{-1, 0, 0, 0};
+  if (a.q_indptr == nullptr) {
+    if (tau < a.num_reqs) f = Request{tau, tau, 1, 0};
+    return f;
+  }
+  const int lane = threadIdx.x & 63;
+  const int tq = tile_tokens(a.group);
+  for (int base = 0; base < a.num_reqs; base += 64) {
+    const int r = base + lane;
+    const int q0 = r < a.num_reqs ? a.q_indptr[r] : 0;
+    const int q1 = r < a.num_reqs ? a.q_indptr[r + 1] : 0;
+    const bool ok = q0 >= 0 && q1 > q0 && q1 <= a.num_queries;
+    const int tiles = ok ? (q1 - q0 + tq - 1) / tq : 0;
+    const int incl = meta::wave_inclusive_scan(tiles);
+    const uint64_t above = __ballot(incl > tau);
+    if (above != 0) {
+      const int at = __ffsll(static_cast<long long>(above)) - 1;
+      f.r = base + at;
+      f.q0 = __builtin_amdgcn_readlane(q0, at);
+      f.ql = __builtin_amdgcn_readlane(q1, at) - f.q0;
+      // the last tiles of a prompt see the most keys: they go first
+      const int first = __builtin_amdgcn_readlane(incl - tiles, at);
+      f.tile = __builtin_amdgcn_readlane(tiles, at) - 1 - (tau - first);
+      return f;
+    }
+    tau -= __builtin_amdgcn_readlane(incl, 63);
+  }
+  return f;
+}
+
+template <bool kBf16>
+__device__ __forceinline__ f32x16 mfma32(u32x4 x, u32x4 y, f32x16 acc) {
+  if constexpr (kBf16) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
+                                                   __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
   } else {
-    const uint32_t code = row[(h * head_dim + d) / 2] >> (4 * (d & 1)) & 15;
-    const float m = (code & 7) < 2 ? 0.5f * (code & 7)
-                                   : __uint_as_float(((code & 7) / 2 + 126) << 23) *
-                                         (code & 1 ? 1.5f : 1.f);
-    return (code & 8 ? -m : m) *
-           e8m0_scale(row[heads * (head_dim / 2) + (h * head_dim + d) / 32]);
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x),
+                                                  __builtin_bit_cast(f16x8, y), acc, 0, 0, 0);
   }
 }
 
-template <bool kBf16, int kKind>
-__global__ __launch_bounds__(64) void simple_kernel(PromptArgs a) {
+// LDS transpose read (ds_read_b64_tr_b16): in each group of 16 lanes, lane 4a + b receives element
+// b of the four 16-bit values addressed by lanes a, a+4, a+8 and a+12 of its group.
+__device__ __forceinline__ i16x4 lds_read_tr16(const uint8_t* lds_addr) {
+  typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (lds_i16x4*)(reinterpret_cast<uintptr_t>(lds_addr)));
+}
+
+// x combined with the value of lane i ^ 32.
+template <bool kMax>
+__device__ __forceinline__ float halves(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  const float a = __uint_as_float(r[0]), b = __uint_as_float(r[1]);
+  return kMax ? fmaxf(a, b) : a + b;
+}
+
+// Whether a 16-bit half of w is an infinity or NaN.
+template <bool kBf16>
+__device__ __forceinline__ bool any_nonfinite(uint32_t w) {
+  constexpr uint32_t e = kBf16 ? 0x7f80u : 0x7c00u;
+  return (w & e) == e || (w & e << 16) == e << 16;
+}
+// w with such halves as zeros.
+template <bool kBf16>
+__device__ __forceinline__ uint32_t only_finite(uint32_t w) {
+  constexpr uint32_t e = kBf16 ? 0x7f80u : 0x7c00u;
+  if ((w & e) == e) w &= 0xffff0000u;
+  if ((w & e << 16) == e << 16) w &= 0xffffu;
+  return w;
+}
+
+template <bool kBf16, int kKind, int kD>
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(kD > 128 ? 1 : 2)))
+void prompt_kernel(PromptArgs a) {
   using Elem = typename Act<kBf16>::elem;
-  __shared__ float q_s[256];
-  const int lane = threadIdx.x;
-  const int heads = a.num_kv_heads * a.group;
-  const int64_t id = blockIdx.x;
-  const int qh = static_cast<int>(id % heads);
-  const int i = static_cast<int>(id / heads % a.max_queries);
-  const int r = static_cast<int>(id / heads / a.max_queries);
-  const int q0 = a.q_indptr != nullptr ? a.q_indptr[r] : r;
-  const int q1 = a.q_indptr != nullptr ? a.q_indptr[r + 1] : r + 1;
-  if (q0 < 0 || q1 > a.num_queries || i >= q1 - q0) return;
-  const int ql = q1 - q0;
-  const int h = qh / a.group;
-  const int D = a.head_dim;
-  const int s0 = a.slot_indptr[r];
-  const int n = a.slot_count != nullptr ? a.slot_count[r] : a.slot_indptr[r + 1] - s0;
-  const bool fixed = s0 < 0 || n < 0 || n > a.max_tokens || ql > a.max_queries;
-  const Elem* q = reinterpret_cast<const Elem*>(a.q);
-  Elem* out = reinterpret_cast<Elem*>(a.out);
-  for (int j = i; j < ql; j += a.max_queries) {   // more than one round only where ql is too large
-    const int64_t at = (int64_t)(q0 + j) * a.q_stride + qh * D;
-    const int64_t to = (int64_t)(q0 + j) * a.out_stride + qh * D;
-    for (int d = lane; d < D; d += 64) q_s[d] = static_cast<float>(q[at + d]);
-    __syncthreads();
-    const uint8_t* kplane = a.kv + (int64_t)(2 * a.layer) * a.plane_bytes;
-    const uint8_t* vplane = kplane + a.plane_bytes;
-    const int64_t p = (int64_t)n - ql + j;
-    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t k0 = 0; !fixed && k0 <= p; k0 += 64) {
-      const int64_t k = k0 + lane;
-      const bool seen = k <= p && (a.window == 0 || k > p - a.window || k < a.sinks);
-      if (__ballot(seen) == 0) continue;
-      const int slot = seen ? a.slots[s0 + k] : 0;
-      const bool bad = static_cast<unsigned>(slot) >= static_cast<unsigned>(a.num_slots);
-      float x = -INFINITY;
-      if (seen) {
-        x = 0.f;
-        const uint8_t* row = kplane + (bad ? 0 : slot) * a.row_bytes;
-        for (int d = 0; d < D; ++d) x += q_s[d] * element<kKind>(row, a.num_kv_heads, D, h, d);
-        x = bad ? __builtin_nanf("") : x * a.scale;
+  constexpr int kKeys = key_tile(kD);
+  constexpr int kTiles = kKeys / 32;        // 32-key score tiles
+  constexpr int kChunks = kD / 16;          // score k-steps
+  constexpr int kDC = kD / 32;              // 32-element value chunks
+  // loads of a step: 16 bytes of a head row each
+  constexpr int kLanes = kKind <= 1 ? kD / 8 : kKind == 2 ? kD / 16 : kD / 32;
+  constexpr int kItems = kKeys * kLanes;    // of K, and as many of V
+  constexpr int kLd = 2 * kItems > kThreads ? 2 * kItems / kThreads : 1;
+  constexpr int kSl = kLd > 1 ? kLd / 2 : 1;     // slots of a thread: K and V rows are the same
+  constexpr int kRowK = kD * 2 + 16;             // LDS bytes per K row: 16-byte reads of 32 rows
+  constexpr int kRowV = kD * 2 + 64;             // and per V row: transpose reads of 4 rows x 64 B
+  constexpr int kBuf = kKeys * (kRowK + kRowV);
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kBuf];
+  __shared__ int nonfinite[2];   // step whose V holds an infinity or NaN, by buffer
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = blockIdx.x % a.num_kv_heads;
+  const int split = blockIdx.y;
+  const Request f = find_request(a, blockIdx.x / a.num_kv_heads);
+  if (f.r < 0) return;
+  const int G = a.group;
+  const int tq = tile_tokens(G);
+  const int i0 = f.tile * tq;
+  const int s0 = a.slot_indptr[f.r];
+  const int n = a.slot_count != nullptr ? a.slot_count[f.r] : a.slot_indptr[f.r + 1] - s0;
+  const bool fixed = s0 < 0 || n < 0 || n > a.max_tokens || f.ql > a.max_queries;
+
+  // ---- this lane's query row, and the keys that the tile's and the wave's rows see
+  const int half = lane >> 5;
+  const int m_row = wave * 32 + (lane & 31);
+  const int tok = m_row / G;
+  const int last = min(i0 + tq, f.ql) - 1;            // last token of the tile
+  const bool real = tok < tq && i0 + tok <= last;
+  const int64_t qrow = f.q0 + min(i0 + tok, last);
+  const int qh = h * G + m_row - tok * G;             // (of a row past the tile: any, not written)
+  const int rank0 = n - f.ql;                         // rank of the request's query 0
+  const int p = real ? rank0 + i0 + tok : -1;
+  const int upper = max(rank0 + last + 1, 0);         // keys [0, upper) matter
+  const int low = a.window > 0 ? max(rank0 + i0 - a.window + 1, 0) : 0;
+  const int sk = min(a.sinks, min(low, upper));       // keys [0, sk) and [low, upper): the list
+  const int skip = low - sk;
+  const int count = fixed ? 0 : sk + max(upper - low, 0);
+  const int steps = (count + kKeys - 1) / kKeys;
+  const int step0 = static_cast<int>((int64_t)steps * split / gridDim.y);
+  const int step1 = static_cast<int>((int64_t)steps * (split + 1) / gridDim.y);
+  const int w_tok0 = i0 + wave * 32 / G;
+  const int w_first = rank0 + w_tok0;                                        // ranks of the wave's
+  const int w_last = rank0 + min(i0 + (wave * 32 + 31) / G, last);           // first and last row
+  const bool w_real = w_tok0 <= last && wave * 32 < tq * G;
+
+  // ---- the query operand: element e of chunk c is value 16 c + 8 half + e of the row
+  u32x4 q[kChunks];
+  {
+    const Elem* src = reinterpret_cast<const Elem*>(a.q) + qrow * a.q_stride +
+                      (int64_t)(real ? qh : h * G) * kD + 8 * half;
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+      q[c] = *reinterpret_cast<const u32x4*>(src + 16 * c);
+      if (a.scale < 0.f) q[c] ^= 0x80008000u;
+      if (a.scale == 0.f) q[c] = u32x4{0, 0, 0, 0};
+    }
+  }
+  // weights are powers of two, with a positive factor (a hidden key's -inf stays one)
+  const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504088896340736f;
+
+  // ---- loads
+  const uint8_t* kplane = a.kv + (int64_t)(2 * a.layer) * a.plane_bytes;
+  // slots of a step's rows: -1 past the list, -2 outside the pool
+  auto load_slots = [&](int j, int (&s)[kSl]) {
+#pragma unroll
+    for (int x = 0; x < kSl; ++x) {
+      const int t = j * kKeys + (tid + x * kThreads) / kLanes % kKeys;
+      const int k = t + (t < sk ? 0 : skip);
+      s[x] = a.slots[(int64_t)s0 + (t < count ? k : 0)];
+      if (static_cast<unsigned>(s[x]) >= static_cast<unsigned>(a.num_slots)) s[x] = -2;
+      if (t >= count) s[x] = -1;
+    }
+  };
+  u32x4 data[kLd];
+  uint32_t exponent[kLd];
+  auto load_rows = [&](const int (&s)[kSl]) {
+#pragma unroll
+    for (int x = 0; x < kLd; ++x) {
+      const int item = tid + x * kThreads;
+      if (2 * kItems < kThreads && item >= 2 * kItems) break;
+      const int slot = max(s[x % kSl], 0);
+      const int ln = item % kLanes;
+      const uint8_t* row =
+          kplane + (item / kItems) * a.plane_bytes + (int64_t)slot * a.row_bytes;
+      data[x] = *reinterpret_cast<const u32x4*>(row + (h * kLanes + ln) * 16);
+      if constexpr (kKind == 3) {
+        exponent[x] = row[a.num_kv_heads * (kD / 2) + h * (kD / 32) + ln];
       }
-      float mi = x;
-      for (int d = 1; d < 64; d <<= 1) mi = fmaxf(mi, __shfl_xor(mi, d, 64));
-      mi = fmaxf(mi, m);
-      const float safe = mi == -INFINITY ? 0.f : mi;
-      const float f = __expf(m - safe);
-      m = mi;
-      const float w = seen ? __expf(x - safe) : 0.f;
-      l = l * f + w;
-      for (int c = 0; c < 4; ++c) o[c] *= f;
-      for (int t = 0; t < 64; ++t) {
-        if (!__shfl(static_cast<int>(seen), t, 64)) continue;
-        const float wt = __shfl(w, t, 64);
-        const int st = __shfl(bad ? 0 : slot, t, 64);
-        const uint8_t* row = vplane + st * a.row_bytes;
-        for (int c = 0; c < 4; ++c) {
-          if (c * 64 + lane < D) o[c] += wt * element<kKind>(row, a.num_kv_heads, D, h, c * 64 + lane);
+    }
+  };
+  // the loaded rows as 16-bit values in LDS
+  auto stage = [&](int j, const int (&s)[kSl], bool look) {
+    uint8_t* buf = lds + (j & 1) * kBuf;
+    bool odd = false;
+#pragma unroll
+    for (int x = 0; x < kLd; ++x) {
+      const int item = tid + x * kThreads;
+      if (2 * kItems < kThreads && item >= 2 * kItems) break;
+      const bool is_v = item >= kItems;
+      const int row = item / kLanes % kKeys;
+      const int ln = item % kLanes;
+      constexpr int kOut = kKind <= 1 ? 1 : kKind == 2 ? 2 : 4;   // 16-byte pieces of LDS
+      u32x4 o[kOut];
+      if constexpr (kKind <= 1) {
+        o[0] = data[x];
+      } else if constexpr (kKind == 2) {
+        o[0] = widen_fp8<kBf16>(u32x2{data[x].x, data[x].y});
+        o[1] = widen_fp8<kBf16>(u32x2{data[x].z, data[x].w});
+      } else {
+        const float e = e8m0_scale(exponent[x]);
+#pragma unroll
+        for (int y = 0; y < 4; ++y) o[y] = widen_fp4(data[x][y], e);
+      }
+      const int slot = s[x % kSl];
+      if (slot < 0) {   // nothing of V; K of a slot outside the pool is NaN to whoever sees it
+        const uint32_t fill = slot == -2 && !is_v ? 0x7fff7fffu : 0u;
+#pragma unroll
+        for (int y = 0; y < kOut; ++y) o[y] = u32x4{fill, fill, fill, fill};
+      }
+      uint8_t* dst = is_v ? buf + kKeys * kRowK + row * kRowV : buf + row * kRowK;
+#pragma unroll
+      for (int y = 0; y < kOut; ++y) {
+        *reinterpret_cast<u32x4*>(dst + (ln * kOut + y) * 16) = o[y];
+        if (look && is_v) {
+#pragma unroll
+          for (int z = 0; z < 4; ++z) odd |= any_nonfinite<kBf16>(o[y][z]);
         }
       }
     }
-    for (int d = 1; d < 64; d <<= 1) l += __shfl_xor(l, d, 64);
-    for (int c = 0; c < 4; ++c) {
-      const int d = c * 64 + lane;
-      if (d >= D) break;
-      out[to + d] = static_cast<Elem>(fixed ? __builtin_nanf("") : l == 0.f ? 0.f : o[c] / l);
+    if (look && odd) nonfinite[j & 1] = j;
+  };
+  // whether every key of step j is seen by all of the rows of ranks [first, last]
+  auto all_seen = [&](int j, int first, int lst) {
+    const int t0 = j * kKeys, t1 = t0 + kKeys - 1;
+    const int kmin = t0 + (t0 < sk ? 0 : skip), kmax = t1 + (t1 < sk ? 0 : skip);
+    return t1 < count && kmax <= first &&
+           (a.window == 0 || kmax < a.sinks || (t0 >= sk && kmin > lst - a.window));
+  };
+
+  float m = -INFINITY, l = 0.f;
+  f32x16 o[kDC];
+#pragma unroll
+  for (int dc = 0; dc < kDC; ++dc)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) o[dc][e] = 0.f;
+
+  auto compute = [&](int j) {
+    const uint8_t* buf = lds + (j & 1) * kBuf;
+    // ---- scores: lane holds keys 32 t + 8 (i / 4) + 4 half + i % 4 of its row
+    f32x16 s[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
+      const uint8_t* src = buf + (32 * t + (lane & 31)) * kRowK + 16 * half;
+#pragma unroll
+      for (int c = 0; c < kChunks; ++c) {
+        s[t] = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(src + 32 * c), q[c], s[t]);
+      }
     }
+    const bool full = all_seen(j, w_first, w_last);
+    auto key_of = [&](int t, int e) {   // rank of the lane's key, or past every row's
+      const int x = j * kKeys + 32 * t + 8 * (e / 4) + 4 * half + e % 4;
+      return x >= count ? INT32_MAX : x + (x < sk ? 0 : skip);
+    };
+    auto seen = [&](int k) {
+      return k <= p && (a.window == 0 || k > p - a.window || k < a.sinks);
+    };
+    if (!full) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          if (!seen(key_of(t, e))) s[t][e] = -INFINITY;
+        }
+    }
+    // ---- weights 2^(x - m); m follows the row's maximum where that passes it by 2^8 (the weights
+    // then stay below 2^8, and the sums so far are seldom scaled)
+    float top = s[0][0];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
+    top = halves<true>(top) * scale;
+    if (__ballot(top > m + 8.f) != 0) {
+      const float to = top > m ? top : m;
+      const float by = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);
+      m = to;
+      l *= by;
+#pragma unroll
+      for (int dc = 0; dc < kDC; ++dc)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[dc][e] *= by;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        s[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], scale, -base));
+        l += s[t][e];
+      }
+    // ---- O^T += V^T . P^T, 16 keys at a time: a lane's weights 8 y .. 8 y + 7 of tile t are keys
+    // 16 y + 4 half + (0..3) and those eight on; the V rows are read in that order
+    const uint8_t* vsrc = buf + kKeys * kRowK + (4 * half + (lane & 15) / 4) * kRowV +
+                          ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    auto product = [&](auto clean) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          typename Act<kBf16>::x8 w;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) w[e] = static_cast<Elem>(s[t][8 * y + e]);
+          const uint8_t* src = vsrc + (32 * t + 16 * y) * kRowV;
+#pragma unroll
+          for (int dc = 0; dc < kDC; ++dc) {
+            const i16x4 x1 = lds_read_tr16(src + dc * 64);
+            const i16x4 x2 = lds_read_tr16(src + 8 * kRowV + dc * 64);
+            const i16x8 xv = {x1[0], x1[1], x1[2], x1[3], x2[0], x2[1], x2[2], x2[3]};
+            u32x4 v = __builtin_bit_cast(u32x4, xv);
+            if constexpr (decltype(clean)::value) {
+#pragma unroll
+              for (int z = 0; z < 4; ++z) v[z] = only_finite<kBf16>(v[z]);
+            }
+            o[dc] = mfma32<kBf16>(v, __builtin_bit_cast(u32x4, w), o[dc]);
+          }
+        }
+    };
+    if (full || nonfinite[j & 1] != j) {
+      product(std::false_type{});
+    } else {
+      // a zero weight times an infinity would be NaN: the product goes without them, and the rows
+      // that see such a value take it as it is
+      product(std::true_type{});
+      for (int x = 0; x < kKeys; ++x) {
+        const int t = j * kKeys + x;
+        const int k = t >= count ? INT32_MAX : t + (t < sk ? 0 : skip);
+        const Elem* row = reinterpret_cast<const Elem*>(buf + kKeys * kRowK + x * kRowV);
+        const bool sees = seen(k);
+#pragma unroll
+        for (int dc = 0; dc < kDC; ++dc)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float v = static_cast<float>(row[32 * dc + 8 * (e / 4) + 4 * half + e % 4]);
+            if (sees && !(fabsf(v) < INFINITY)) o[dc][e] += v;
+          }
+      }
+    }
+  };
+
+  if (tid < 2) nonfinite[tid] = -1;
+  int sa[kSl], sb[kSl];
+  if (step0 < step1) {
+    load_slots(step0, sa);
+    load_rows(sa);
+    load_slots(step0 + 1, sb);
+  }
+  __syncthreads();
+  for (int j = step0; j < step1; ++j) {
+    stage(j, sa, !all_seen(j, rank0 + i0, rank0 + last));
+    if (j + 1 < step1) {
+#pragma unroll
+      for (int x = 0; x < kSl; ++x) sa[x] = sb[x];
+      load_rows(sa);
+      load_slots(j + 2, sb);
+    }
+    // one barrier a step: buffer j & 1 was last read two steps ago, before the last barrier
     __syncthreads();
+    const int k0 = j * kKeys + (j * kKeys < sk ? 0 : skip);
+    if (w_real && k0 <= w_last) compute(j);
+  }
+
+  // ---- the rows' results: lane holds values 32 dc + 8 (e / 4) + 4 half + e % 4
+  if (!real) return;
+  l = halves<false>(l);
+  if (gridDim.y == 1) {
+    const float inv = fixed ? __builtin_nanf("") : l == 0.f ? 0.f : 1.f / l;
+    Elem* dst = reinterpret_cast<Elem*>(a.out) + qrow * a.out_stride + (int64_t)qh * kD + 4 * half;
+    typedef Elem Elem4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int dc = 0; dc < kDC; ++dc)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const Elem4 w = {static_cast<Elem>(o[dc][4 * e] * inv),
+                         static_cast<Elem>(o[dc][4 * e + 1] * inv),
+                         static_cast<Elem>(o[dc][4 * e + 2] * inv),
+                         static_cast<Elem>(o[dc][4 * e + 3] * inv)};
+        *reinterpret_cast<Elem4*>(dst + 32 * dc + 8 * e) = w;
+      }
+    return;
+  }
+  float* rec = a.workspace +
+               ((qrow * a.num_kv_heads * G + qh) * gridDim.y + split) * (kD + 2);
+  if (half == 0) {
+    rec[0] = fixed ? __builtin_nanf("") : m;
+    rec[1] = l;
+  }
+#pragma unroll
+  for (int dc = 0; dc < kDC; ++dc)
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      *reinterpret_cast<f32x4_in*>(rec + 2 + 32 * dc + 8 * e + 4 * half) =
+          f32x4{o[dc][4 * e], o[dc][4 * e + 1], o[dc][4 * e + 2], o[dc][4 * e + 3]};
+}
+
+// Merges the split records (m, l, O) of a tile's rows: weights 2^(m_s - max m).
+template <bool kBf16>
+__global__ __launch_bounds__(kThreads) void combine_kernel(PromptArgs a, int splits) {
+  using Elem = typename Act<kBf16>::elem;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int h = blockIdx.x % a.num_kv_heads;
+  const Request f = find_request(a, blockIdx.x / a.num_kv_heads);
+  if (f.r < 0) return;
+  const int G = a.group, D = a.head_dim;
+  const int tq = tile_tokens(G);
+  const int tokens = min(tq, f.ql - f.tile * tq);
+  for (int row = blockIdx.y * kWaves + wave; row < tokens * G; row += gridDim.y * kWaves) {
+    const int64_t qrow = f.q0 + f.tile * tq + row / G;
+    const int qh = h * G + row % G;
+    const float* rec = a.workspace + (qrow * a.num_kv_heads * G + qh) * splits * (D + 2);
+    const bool mine = lane < splits;
+    const float ms = mine ? rec[(int64_t)lane * (D + 2)] : -INFINITY;
+    const float ls = mine ? rec[(int64_t)lane * (D + 2) + 1] : 0.f;
+    float top = ms;
+    const bool nan = __ballot(ms != ms) != 0;
+    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+    const float w = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - top);
+    float total = ls * w;
+    for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d, 64);
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < splits; ++s) {
+      const float ws = __shfl(w, s, 64);
+      if (ws == 0.f) continue;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        if (c * 64 + lane < D) v[c] += ws * rec[(int64_t)s * (D + 2) + 2 + c * 64 + lane];
+      }
+    }
+    const float inv = nan ? __builtin_nanf("") : total == 0.f ? 0.f : 1.f / total;
+    Elem* dst = reinterpret_cast<Elem*>(a.out) + qrow * a.out_stride + (int64_t)qh * D;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      if (c * 64 + lane < D) dst[c * 64 + lane] = static_cast<Elem>(v[c] * inv);
+    }
+  }
+}
+
+// Tiles of query rows that a batch can have.
+int64_t most_tiles(const PromptArgs& a) {
+  if (a.q_indptr == nullptr) return a.num_reqs;
+  const int tq = tile_tokens(a.group);
+  const int64_t by_rows = a.num_queries / tq + (int64_t)a.num_reqs;
+  const int64_t by_reqs = (int64_t)a.num_reqs * ((a.max_queries + tq - 1) / tq);
+  return by_rows < by_reqs ? by_rows : by_reqs;
+}
+
+int prompt_splits(const PromptArgs& a) {
+  const int64_t groups = most_tiles(a) * a.num_kv_heads;
+  if (groups == 0) return 1;
+  int64_t keys = a.max_tokens;
+  if (a.window > 0) {
+    const int64_t list = (int64_t)a.window + a.sinks + tile_tokens(a.group);
+    keys = list < keys ? list : keys;
+  }
+  const int64_t steps = (keys + key_tile(a.head_dim) - 1) / key_tile(a.head_dim);
+  const int64_t want = (512 + groups - 1) / groups;      // workgroups: two per CU
+  int64_t splits = want < steps / 4 ? want : steps / 4;  // at least four steps each
+  if (splits > kMaxSplits) splits = kMaxSplits;
+  return splits < 1 ? 1 : static_cast<int>(splits);
+}
+
+template <bool kBf16, int kKind>
+auto pick_prompt(int head_dim) -> void (*)(PromptArgs) {
+  switch (head_dim) {
+    case 32: return prompt_kernel<kBf16, kKind, 32>;
+    case 64: return prompt_kernel<kBf16, kKind, 64>;
+    case 128: return prompt_kernel<kBf16, kKind, 128>;
+    case 256: return prompt_kernel<kBf16, kKind, 256>;
+    default: return nullptr;
   }
 }
 
 }  // namespace
 
-int64_t prompt_workspace_bytes(const PromptArgs& a, int kind) { return 0; }
+int64_t prompt_workspace_bytes(const PromptArgs& a, int kind) {
+  const int splits = prompt_splits(a);
+  if (splits == 1) return 0;
+  return (int64_t)a.num_queries * a.num_kv_heads * a.group * splits * (a.head_dim + 2) * 4;
+}
 
 hipError_t launch_prompt(const PromptArgs& a, bool bf16, int kind, hipStream_t stream) {
-  const int64_t grid = (int64_t)a.num_reqs * a.max_queries * a.num_kv_heads * a.group;
-  if (grid > INT32_MAX) return hipErrorInvalidValue;
+  const int64_t groups = most_tiles(a) * a.num_kv_heads;
+  if (groups > INT32_MAX) return hipErrorInvalidValue;
+  if (groups == 0) return hipSuccess;
   void (*kernel)(PromptArgs) = nullptr;
   switch (kind) {
-    case 0: kernel = simple_kernel<false, 0>; break;
-    case 1: kernel = simple_kernel<true, 1>; break;
-    case 2: kernel = bf16 ? simple_kernel<true, 2> : simple_kernel<false, 2>; break;
-    case 3: kernel = simple_kernel<true, 3>; break;
-    default: return hipErrorInvalidValue;
+    case 0: kernel = pick_prompt<false, 0>(a.head_dim); break;
+    case 1: kernel = pick_prompt<true, 1>(a.head_dim); break;
+    case 2: kernel = bf16 ? pick_prompt<true, 2>(a.head_dim) : pick_prompt<false, 2>(a.head_dim); break;
+    case 3: kernel = pick_prompt<true, 3>(a.head_dim); break;
+    default: break;
   }
-  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(grid)), dim3(64), 0, stream, a);
+  if (kernel == nullptr) return hipErrorInvalidValue;
+  const int splits = prompt_splits(a);
+  hipLaunchKernelGGL(kernel, dim3(static_cast<unsigned>(groups), splits), dim3(kThreads), 0, stream,
+                     a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || splits == 1) return e;
+  const unsigned parts = a.max_queries * a.group > 32 ? 8 : 1;
+  hipLaunchKernelGGL(bf16 ? combine_kernel<true> : combine_kernel<false>,
+                     dim3(static_cast<unsigned>(groups), parts), dim3(kThreads), 0, stream, a,
+                     splits);
   return hipGetLastError();
 }
 
