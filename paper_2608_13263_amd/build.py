@@ -22,7 +22,7 @@ CSRC = os.path.join(HERE, "csrc")
 SOURCES = [os.path.join(CSRC, f)
            for f in ("vtoken_abi.hip", "vtoken_kernels.hip", "vtoken_copy.hip",
                      "vtoken_attention.hip", "vtoken_planner.hip", "vtoken_layout.hip",
-                     "vtoken_rows.hip", "vtoken_prompt.hip")]
+                     "vtoken_rows.hip", "vtoken_prompt.hip", "vtoken_single.hip")]
 HEADERS = [os.path.join(ROOT, "include", "vtoken.h"), os.path.join(CSRC, "vtoken_internal.h")]
 ARCH = "gfx950"
 

@@ -779,7 +779,8 @@ extern "C" {
 int64_t vtoken_attention_workspace_bytes(const vtoken_attention* t, int32_t num_reqs) {
   vtoken::PromptArgs a;
   if (t == nullptr || attention_sizes(t, num_reqs, &a) != VTOKEN_OK) return -1;
-  return vtoken::prompt_workspace_bytes(a, t->kv_dtype);
+  return a.max_queries == 1 ? vtoken::single_workspace_bytes(a, t->kv_dtype)
+                            : vtoken::prompt_workspace_bytes(a, t->kv_dtype);
 }
 
 vtoken_status vtoken_paged_attention(const vtoken_cache* cache, const vtoken_attention* t,
@@ -817,8 +818,9 @@ vtoken_status vtoken_paged_attention(const vtoken_cache* cache, const vtoken_att
   a.slot_count = t->slot_count;
   a.workspace = t->workspace;
   a.num_slots = cache->num_blocks * cache->block_size;
-  return hip_status(
-      vtoken::launch_prompt(a, t->dtype == VTOKEN_KV_BF16, t->kv_dtype, stream));
+  const bool bf16 = t->dtype == VTOKEN_KV_BF16;
+  return hip_status(a.max_queries == 1 ? vtoken::launch_single(a, bf16, t->kv_dtype, stream)
+                                       : vtoken::launch_prompt(a, bf16, t->kv_dtype, stream));
 }
 
 int64_t vtoken_check_layout_workspace_bytes(int32_t num_blocks) {

@@ -20,6 +20,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 // the same in a caller's float buffers, which are aligned to a float and no more
 typedef f32x2 f32x2_in __attribute__((aligned(4)));
 typedef f32x4 f32x4_in __attribute__((aligned(4)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
 
 // The 16-bit type of activations and of matrix-core operands.
 template <bool kBf16>
@@ -70,6 +72,14 @@ __device__ __forceinline__ u32x4 widen_fp4(uint32_t w, float scale) {
   o.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2));
   o.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3));
   return o;
+}
+
+// LDS transpose read (ds_read_b64_tr_b16): in each group of 16 lanes, lane 4a + b receives element
+// b of the four 16-bit values addressed by lanes a, a+4, a+8 and a+12 of its group.
+__device__ __forceinline__ i16x4 lds_read_tr16(const uint8_t* lds_addr) {
+  typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (lds_i16x4*)(reinterpret_cast<uintptr_t>(lds_addr)));
 }
 
 }  // namespace elements

@@ -1,5 +1,6 @@
 // Internal declarations shared by the kernels (vtoken_kernels.hip, vtoken_copy.hip,
-// vtoken_attention.hip, vtoken_planner.hip, vtoken_layout.hip, vtoken_rows.hip, vtoken_prompt.hip) and the C ABI front end
+// vtoken_attention.hip, vtoken_planner.hip, vtoken_layout.hip, vtoken_rows.hip, vtoken_prompt.hip,
+// vtoken_single.hip) and the C ABI front end
 // (vtoken_abi.hip). Not installed; the public interface is include/vtoken.h.
 #pragma once
 
@@ -448,6 +449,9 @@ struct PromptArgs {
 };
 int64_t prompt_workspace_bytes(const PromptArgs& a, int kind);
 hipError_t launch_prompt(const PromptArgs& a, bool bf16, int kind, hipStream_t stream);
+// The same where no request has more than one query (vtoken_single.hip).
+int64_t single_workspace_bytes(const PromptArgs& a, int kind);
+hipError_t launch_single(const PromptArgs& a, bool bf16, int kind, hipStream_t stream);
 
 hipError_t launch_build(const MetaArgs& a, hipStream_t stream);
 // variant: 0 default (4), 1 LDS double buffer, 2 LDS single buffer, 3 registers, 4 row walk

@@ -17,8 +17,6 @@ namespace {
 using namespace elements;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef short i16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
@@ -81,14 +79,6 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 x, u32x4 y, f32x16 acc) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, x),
                                                   __builtin_bit_cast(f16x8, y), acc, 0, 0, 0);
   }
-}
-
-// LDS transpose read (ds_read_b64_tr_b16): in each group of 16 lanes, lane 4a + b receives element
-// b of the four 16-bit values addressed by lanes a, a+4, a+8 and a+12 of its group.
-__device__ __forceinline__ i16x4 lds_read_tr16(const uint8_t* lds_addr) {
-  typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (lds_i16x4*)(reinterpret_cast<uintptr_t>(lds_addr)));
 }
 
 // x combined with the value of lane i ^ 32.
