@@ -728,15 +728,19 @@ def rotary_table(num_positions: int, rotary_dim: int, base: float = 10000.0, dev
     return torch.cat([angle.cos(), angle.sin()], 1).float()
 
 
-def _activation(x, name: str, device, dtype, heads: int, head_dim: int) -> int:
+def _activation(x, name: str, device, dtype, heads: int, head_dim: int, rows: int = 0) -> int:
     """A [tokens][heads][head_dim] activation tensor's stride between tokens, in elements."""
-    if x.dim() != 3 or x.shape[1] != heads or x.shape[2] != head_dim:
+    shape = x.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != head_dim:
         raise ValueError(f"{name} must be [tokens][{heads}][{head_dim}]")
     if x.dtype != dtype or x.device != device:
         raise ValueError(f"{name} must be {dtype} on {device}")
-    if (heads > 1 and x.stride(1) != head_dim) or x.stride(2) != 1:
+    stride, across, step = x.stride()
+    if (heads > 1 and across != head_dim) or step != 1:
         raise ValueError(f"the heads of a token must be contiguous in {name}")
-    return x.stride(0) if x.shape[0] > 1 else heads * head_dim
+    if shape[0] < rows:
+        raise ValueError(f"{name} must have a row for every slot")
+    return stride if shape[0] > 1 else heads * head_dim
 
 
 def _ints(x, name: str, device, numel: Optional[int] = None) -> None:
@@ -763,13 +767,22 @@ def _cache_code(cache: KVCache, kv_dtype) -> int:
     return kv_dtype_code(cache.kv.dtype) if code is None else code
 
 
-def _on_device(device, stream, call):
-    """call(stream) with the tensors' device current, on `stream` or that device's current one."""
+def _enqueue(fn, where: str, device, stream, *args) -> None:
+    """fn(*args, stream) with the tensors' device current, on `stream` or that device's current
+    one."""
     import torch
-    if device.index is None or device.index == torch.cuda.current_device():
-        return call(_stream(stream))
-    with torch.cuda.device(device):
-        return call(_stream(stream))
+    index = device.index
+    if stream is None:   # (a Stream object costs more than the rest of a small call)
+        raw = torch._C._cuda_getCurrentRawStream(index)
+    else:
+        raw = _stream(stream)
+    if index == torch._C._cuda_getDevice():
+        status = fn(*args, raw)
+    else:
+        with torch.cuda.device(device):
+            status = fn(*args, raw)
+    if status != VTOKEN_OK:
+        _check(status, where)
 
 
 def write_kv(cache: KVCache, k, v, slots, layer: int, q=None, positions=None, cos_sin=None,
@@ -782,34 +795,22 @@ def write_kv(cache: KVCache, k, v, slots, layer: int, q=None, positions=None, co
     Returns q_out (q may be given for it), or None without q; rows of padding tokens in a q_out
     made here are not set."""
     import torch
-    lib = load_library()
     dev = cache.kv.device
-    H, D, n = cache.num_kv_heads, cache.head_dim, int(slots.numel())
+    H, D, n, act = cache.num_kv_heads, cache.head_dim, slots.numel(), k.dtype
     _ints(slots, "slots", dev)
-    w = CKVWrite(num_tokens=n, num_kv_heads=H, head_dim=D, layer=int(layer), eps=float(eps),
-                 interleaved=int(bool(interleaved)), dtype=_act_code(k.dtype),
-                 kv_dtype=_cache_code(cache, kv_dtype), slots=_ptr(slots), k=_ptr(k), v=_ptr(v),
-                 k_stride=_activation(k, "k", dev, k.dtype, H, D),
-                 v_stride=_activation(v, "v", dev, k.dtype, H, D))
-    if k.shape[0] < n or v.shape[0] < n:
-        raise ValueError("k and v must have a row for every slot")
+    q_heads = q_stride = out_stride = rotary = num_positions = 0
     if q is not None:
-        heads = int(q.shape[1]) if q.dim() == 3 else 0
-        w.num_q_heads, w.q = heads, _ptr(q)
-        w.q_stride = _activation(q, "q", dev, k.dtype, heads, D)
+        q_heads = int(q.shape[1]) if q.dim() == 3 else 0
+        q_stride = _activation(q, "q", dev, act, q_heads, D, n)
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-        w.q_out, w.q_out_stride = _ptr(q_out), _activation(q_out, "q_out", dev, k.dtype, heads, D)
-        if q.shape[0] < n or q_out.shape[0] < n:
-            raise ValueError("q and q_out must have a row for every slot")
+            q_out = torch.empty(q.shape, dtype=act, device=dev)
+        out_stride = _activation(q_out, "q_out", dev, act, q_heads, D, n)
     elif q_out is not None:
         raise ValueError("q_out without q")
     for name, x in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if x is not None:
-            if x.dtype != torch.float32 or x.device != dev or x.shape != (D,) or \
-                    not x.is_contiguous():
-                raise ValueError(f"{name} must be float32 [{D}] on {dev}")
-            setattr(w, name, _ptr(x))
+        if x is not None and (x.dtype != torch.float32 or x.device != dev or x.shape != (D,) or
+                              not x.is_contiguous()):
+            raise ValueError(f"{name} must be float32 [{D}] on {dev}")
     if cos_sin is not None:
         if positions is None:
             raise ValueError("a table needs positions")
@@ -817,11 +818,14 @@ def write_kv(cache: KVCache, k, v, slots, layer: int, q=None, positions=None, co
                 not cos_sin.is_contiguous():
             raise ValueError(f"cos_sin must be contiguous float32 [positions][rotary_dim] on {dev}")
         _ints(positions, "positions", dev, n)
-        w.cos_sin, w.positions = _ptr(cos_sin), _ptr(positions)
-        w.num_positions, w.rotary_dim = int(cos_sin.shape[0]), int(cos_sin.shape[1])
-    c = cache.c()
-    _check(_on_device(dev, stream, lambda st: lib.vtoken_write_kv(
-        ctypes.byref(c), ctypes.byref(w), st)), "vtoken_write_kv")
+        num_positions, rotary = cos_sin.shape
+    w = CKVWrite(_ptr(q), k.data_ptr(), v.data_ptr(), _ptr(q_out), q_stride,
+                 _activation(k, "k", dev, act, H, D, n), _activation(v, "v", dev, act, H, D, n),
+                 out_stride, _ptr(q_weight), _ptr(k_weight), _ptr(cos_sin), _ptr(positions),
+                 slots.data_ptr(), n, q_heads, H, D, rotary, num_positions,
+                 1 if interleaved else 0, layer, _act_code(act), _cache_code(cache, kv_dtype), eps)
+    _enqueue(load_library().vtoken_write_kv, "vtoken_write_kv", dev, stream,
+             ctypes.byref(cache.c()), ctypes.byref(w))
     return q_out
 
 
@@ -831,9 +835,8 @@ def read_kv(cache: KVCache, slots, layer: int, dtype=None, k_out=None, v_out=Non
     [n][num_kv_heads][head_dim] tensors (k, v), fp16 or bf16 (`dtype`; by default the cache's own
     type, bf16 for fp8 and 4-bit caches)."""
     import torch
-    lib = load_library()
     dev = cache.kv.device
-    H, D, n = cache.num_kv_heads, cache.head_dim, int(slots.numel())
+    H, D, n = cache.num_kv_heads, cache.head_dim, slots.numel()
     _ints(slots, "slots", dev)
     code = _cache_code(cache, kv_dtype)
     if dtype is None:
@@ -843,16 +846,12 @@ def read_kv(cache: KVCache, slots, layer: int, dtype=None, k_out=None, v_out=Non
         k_out = torch.empty(n, H, D, dtype=dtype, device=dev)
     if v_out is None:
         v_out = torch.empty(n, H, D, dtype=dtype, device=dev)
-    r = CKVRead(slots=_ptr(slots), k_out=_ptr(k_out), v_out=_ptr(v_out),
-                k_stride=_activation(k_out, "k_out", dev, dtype, H, D),
-                v_stride=_activation(v_out, "v_out", dev, dtype, H, D), num_tokens=n,
-                num_kv_heads=H, head_dim=D, layer=int(layer), dtype=_act_code(dtype),
-                kv_dtype=code)
-    if k_out.shape[0] < n or v_out.shape[0] < n:
-        raise ValueError("k_out and v_out must have a row for every slot")
-    c = cache.c()
-    _check(_on_device(dev, stream, lambda st: lib.vtoken_read_kv(
-        ctypes.byref(c), ctypes.byref(r), st)), "vtoken_read_kv")
+    r = CKVRead(slots.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
+                _activation(k_out, "k_out", dev, dtype, H, D, n),
+                _activation(v_out, "v_out", dev, dtype, H, D, n), n, H, D, layer,
+                _act_code(dtype), code)
+    _enqueue(load_library().vtoken_read_kv, "vtoken_read_kv", dev, stream,
+             ctypes.byref(cache.c()), ctypes.byref(r))
     return k_out, v_out
 
 
@@ -874,33 +873,31 @@ def paged_attention(cache: KVCache, q, slot_indptr, slots, layer: int, max_token
     max_tokens and max_queries bound every request's slots and queries (max_queries: by default
     the number of rows of q). Rows of q past the last query are left alone."""
     import torch
-    lib = load_library()
     dev = cache.kv.device
-    D = cache.head_dim
+    D, act = cache.head_dim, q.dtype
     heads = int(q.shape[1]) if q.dim() == 3 else 0
     _ints(slot_indptr, "slot_indptr", dev, 1)
     _ints(slots, "slots", dev)
-    R = int(slot_indptr.numel()) - 1
-    stride = _activation(q, "q", dev, q.dtype, heads, D)
+    R, rows = slot_indptr.numel() - 1, int(q.shape[0])
+    stride = _activation(q, "q", dev, act, heads, D)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
-    if out.shape != q.shape:
+        out = torch.empty(q.shape, dtype=act, device=dev)
+    elif out.shape != q.shape:
         raise ValueError("out must match q")
     if q_indptr is not None:
         _ints(q_indptr, "q_indptr", dev, R + 1)
     if slot_count is not None:
         _ints(slot_count, "slot_count", dev, R)
     if max_queries is None:
-        max_queries = 1 if q_indptr is None else int(q.shape[0])
-    a = CAttention(
-        q=_ptr(q), out=_ptr(out), q_stride=stride,
-        out_stride=_activation(out, "out", dev, q.dtype, heads, D), q_indptr=_ptr(q_indptr),
-        slot_count=_ptr(slot_count), num_queries=int(q.shape[0]), max_queries=int(max_queries),
-        max_tokens=int(max_tokens), num_q_heads=heads, num_kv_heads=cache.num_kv_heads,
-        head_dim=D, layer=int(layer), dtype=_act_code(q.dtype),
-        kv_dtype=_cache_code(cache, kv_dtype), window=int(window), sinks=int(sinks),
-        scale=float(D ** -0.5 if scale is None else scale))
-    need = attention_workspace_bytes(a, R)
+        max_queries = 1 if q_indptr is None else rows
+    a = CAttention(q.data_ptr(), out.data_ptr(), stride,
+                   _activation(out, "out", dev, act, heads, D), _ptr(q_indptr), _ptr(slot_count),
+                   0, 0, rows, max_queries, max_tokens, heads, cache.num_kv_heads, D, layer,
+                   _act_code(act), _cache_code(cache, kv_dtype), window, sinks,
+                   D ** -0.5 if scale is None else scale)
+    lib = load_library()
+    ref = ctypes.byref(a)
+    need = lib.vtoken_attention_workspace_bytes(ref, R)   # (-1: the call itself says why)
     if workspace is None and need > 0:
         workspace = torch.empty((need + 3) // 4, dtype=torch.float32, device=dev)
         if stream is not None and hasattr(stream, "cuda_stream"):
@@ -908,10 +905,8 @@ def paged_attention(cache: KVCache, q, slot_indptr, slots, layer: int, max_token
     if workspace is not None:
         if workspace.device != dev or not workspace.is_contiguous():
             raise ValueError(f"workspace must be contiguous on {dev}")
-        a.workspace = _ptr(workspace)
-        a.workspace_bytes = int(workspace.numel() * workspace.element_size())
-    c = cache.c()
-    _check(_on_device(dev, stream, lambda st: lib.vtoken_paged_attention(
-        ctypes.byref(c), ctypes.byref(a), R, _ptr(slot_indptr), _ptr(slots), st)),
-        "vtoken_paged_attention")
+        a.workspace = workspace.data_ptr()
+        a.workspace_bytes = workspace.numel() * workspace.element_size()
+    _enqueue(lib.vtoken_paged_attention, "vtoken_paged_attention", dev, stream,
+             ctypes.byref(cache.c()), ref, R, slot_indptr.data_ptr(), slots.data_ptr())
     return out

@@ -423,10 +423,12 @@ void prompt_kernel(PromptArgs a) {
           f32x4{o[dc][4 * e], o[dc][4 * e + 1], o[dc][4 * e + 2], o[dc][4 * e + 3]};
 }
 
-// Merges the split records (m, l, O) of a tile's rows: weights 2^(m_s - max m).
+// Merges the split records (m, l, O) of a tile's rows, a row per wave: weights 2^(m_s - max m).
+// Bound: latency; every wave reads all the (m_s, l_s) at once and eight records at a time.
 template <bool kBf16>
 __global__ __launch_bounds__(kThreads) void combine_kernel(PromptArgs a, int splits) {
   using Elem = typename Act<kBf16>::elem;
+  typedef Elem Elem2 __attribute__((ext_vector_type(2)));
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.x % a.num_kv_heads;
@@ -435,34 +437,51 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(PromptArgs a, int spl
   const int G = a.group, D = a.head_dim;
   const int tq = tile_tokens(G);
   const int tokens = min(tq, f.ql - f.tile * tq);
-  for (int row = blockIdx.y * kWaves + wave; row < tokens * G; row += gridDim.y * kWaves) {
-    const int64_t qrow = f.q0 + f.tile * tq + row / G;
-    const int qh = h * G + row % G;
-    const float* rec = a.workspace + (qrow * a.num_kv_heads * G + qh) * splits * (D + 2);
-    const bool mine = lane < splits;
-    const float ms = mine ? rec[(int64_t)lane * (D + 2)] : -INFINITY;
-    const float ls = mine ? rec[(int64_t)lane * (D + 2) + 1] : 0.f;
-    float top = ms;
-    const bool nan = __ballot(ms != ms) != 0;
-    for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-    const float w = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - top);
-    float total = ls * w;
-    for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d, 64);
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < splits; ++s) {
-      const float ws = __shfl(w, s, 64);
+  const int row = blockIdx.y * kWaves + wave;
+  if (row >= tokens * G) return;
+  const int64_t qrow = f.q0 + f.tile * tq + row / G;
+  const int qh = h * G + row % G;
+  const int64_t rs = D + 2;
+  const float* rec = a.workspace + (qrow * a.num_kv_heads * G + qh) * splits * rs;
+  const f32x2 ml = lane < splits ? *reinterpret_cast<const f32x2_in*>(rec + lane * rs)
+                                 : f32x2{-INFINITY, 0.f};
+  const bool nan = __ballot(ml.x != ml.x) != 0;
+  float top = ml.x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
+  // (a split whose scores are all NaN has no maximum, but a sum)
+  const float w = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f)
+                                    : __builtin_amdgcn_exp2f(ml.x - top);
+  float total = w == 0.f ? 0.f : ml.y * w;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d, 64);
+  const int p0 = 2 * lane, p1 = 128 + 2 * lane;   // this lane's pairs of values
+  f32x2 v0 = {0.f, 0.f}, v1 = {0.f, 0.f};
+  for (int s = 0; s < splits; s += 8) {
+    f32x2 x0[8], x1[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float* src = rec + (s + j < splits ? s + j : s) * rs + 2;
+      x0[j] = p0 < D ? *reinterpret_cast<const f32x2_in*>(src + p0) : f32x2{0.f, 0.f};
+      x1[j] = p1 < D ? *reinterpret_cast<const f32x2_in*>(src + p1) : f32x2{0.f, 0.f};
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float ws = s + j < splits ? __shfl(w, (s + j) & 63, 64) : 0.f;
       if (ws == 0.f) continue;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        if (c * 64 + lane < D) v[c] += ws * rec[(int64_t)s * (D + 2) + 2 + c * 64 + lane];
-      }
+      v0 += x0[j] * ws;
+      v1 += x1[j] * ws;
     }
-    const float inv = nan ? __builtin_nanf("") : total == 0.f ? 0.f : 1.f / total;
-    Elem* dst = reinterpret_cast<Elem*>(a.out) + qrow * a.out_stride + (int64_t)qh * D;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      if (c * 64 + lane < D) dst[c * 64 + lane] = static_cast<Elem>(v[c] * inv);
-    }
+  }
+  const float inv = nan ? __builtin_nanf("") : total == 0.f ? 0.f : 1.f / total;
+  Elem* dst = reinterpret_cast<Elem*>(a.out) + qrow * a.out_stride + (int64_t)qh * D;
+  if (p0 < D) {
+    *reinterpret_cast<Elem2*>(dst + p0) =
+        Elem2{static_cast<Elem>(v0.x * inv), static_cast<Elem>(v0.y * inv)};
+  }
+  if (p1 < D) {
+    *reinterpret_cast<Elem2*>(dst + p1) =
+        Elem2{static_cast<Elem>(v1.x * inv), static_cast<Elem>(v1.y * inv)};
   }
 }
 
@@ -527,7 +546,8 @@ hipError_t launch_prompt(const PromptArgs& a, bool bf16, int kind, hipStream_t s
                      a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || splits == 1) return e;
-  const unsigned parts = a.max_queries * a.group > 32 ? 8 : 1;
+  const int64_t rows = (int64_t)a.max_queries * a.group;
+  const unsigned parts = ((rows < kRows ? static_cast<unsigned>(rows) : kRows) + kWaves - 1) / kWaves;
   hipLaunchKernelGGL(bf16 ? combine_kernel<true> : combine_kernel<false>,
                      dim3(static_cast<unsigned>(groups), parts), dim3(kThreads), 0, stream, a,
                      splits);
