@@ -17,6 +17,10 @@ namespace {
 using namespace elements;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+// LDS addresses, 32 bits wide
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
@@ -90,19 +94,27 @@ __device__ __forceinline__ float halves(float x) {
   return kMax ? fmaxf(a, b) : a + b;
 }
 
-// Whether a 16-bit half of w is an infinity or NaN.
-template <bool kBf16>
-__device__ __forceinline__ bool any_nonfinite(uint32_t w) {
-  constexpr uint32_t e = kBf16 ? 0x7f80u : 0x7c00u;
-  return (w & e) == e || (w & e << 16) == e << 16;
-}
-// w with such halves as zeros.
+// w with 16-bit halves that are infinities or NaN as zeros.
 template <bool kBf16>
 __device__ __forceinline__ uint32_t only_finite(uint32_t w) {
   constexpr uint32_t e = kBf16 ? 0x7f80u : 0x7c00u;
   if ((w & e) == e) w &= 0xffff0000u;
   if ((w & e << 16) == e << 16) w &= 0xffffu;
   return w;
+}
+
+// K and V rows lie in LDS without padding (the loads that write it directly leave none), 16-byte
+// piece c of row r at c ^ swizzle(r): the 16-byte reads of 16 rows at one c, and the transpose
+// reads of 4 rows x 64 bytes, then fall on different banks.
+template <int kD>
+__device__ __forceinline__ int swizzle(int r) {
+  if constexpr (kD >= 128) return (r & 3) << 2 | (r >> 2 & 3);
+  if constexpr (kD == 64) return (r >> 1 & 1) << 2 | (r >> 2 & 3);
+  return r >> 2 & 3;
+}
+template <int kD>
+__device__ __forceinline__ int piece_at(int r, int c) {   // byte offset
+  return r * (kD * 2) + ((c ^ swizzle<kD>(r)) << 4);
 }
 
 template <bool kBf16, int kKind, int kD>
@@ -114,16 +126,18 @@ void prompt_kernel(PromptArgs a) {
   constexpr int kTiles = kKeys / 32;        // 32-key score tiles
   constexpr int kChunks = kD / 16;          // score k-steps
   constexpr int kDC = kD / 32;              // 32-element value chunks
+  // 16-bit rows go straight to LDS, others through registers, where they are widened
+  constexpr bool kDirect = kKind <= 1;
+  constexpr int kRow = kD * 2;              // bytes of a row in LDS
   // loads of a step: 16 bytes of a head row each
   constexpr int kLanes = kKind <= 1 ? kD / 8 : kKind == 2 ? kD / 16 : kD / 32;
   constexpr int kItems = kKeys * kLanes;    // of K, and as many of V
   constexpr int kLd = 2 * kItems > kThreads ? 2 * kItems / kThreads : 1;
   constexpr int kSl = kLd > 1 ? kLd / 2 : 1;     // slots of a thread: K and V rows are the same
-  constexpr int kRowK = kD * 2 + 16;             // LDS bytes per K row: 16-byte reads of 32 rows
-  constexpr int kRowV = kD * 2 + 64;             // and per V row: transpose reads of 4 rows x 64 B
-  constexpr int kBuf = kKeys * (kRowK + kRowV);
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2 * kBuf];
-  __shared__ int nonfinite[2];   // step whose V holds an infinity or NaN, by buffer
+  // two buffers of K rows, then V rows; two objects, so that a read of one is known not to wait
+  // for the loads into the other
+  __shared__ __attribute__((aligned(1024))) uint8_t lds0[2 * kKeys * kRow];
+  __shared__ __attribute__((aligned(1024))) uint8_t lds1[2 * kKeys * kRow];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -190,9 +204,9 @@ void prompt_kernel(PromptArgs a) {
       if (t >= count) s[x] = -1;
     }
   };
-  u32x4 data[kLd];
-  uint32_t exponent[kLd];
-  auto load_rows = [&](const int (&s)[kSl]) {
+  u32x4 data[kDirect ? 1 : kLd];
+  uint32_t exponent[kKind == 3 ? kLd : 1];
+  auto load_rows = [&](const int (&s)[kSl], lds_u8* buf) {
 #pragma unroll
     for (int x = 0; x < kLd; ++x) {
       const int item = tid + x * kThreads;
@@ -201,16 +215,32 @@ void prompt_kernel(PromptArgs a) {
       const int ln = item % kLanes;
       const uint8_t* row =
           kplane + (item / kItems) * a.plane_bytes + (int64_t)slot * a.row_bytes;
-      data[x] = *reinterpret_cast<const u32x4*>(row + (h * kLanes + ln) * 16);
-      if constexpr (kKind == 3) {
-        exponent[x] = row[a.num_kv_heads * (kD / 2) + h * (kD / 32) + ln];
+      if constexpr (kDirect) {
+        // a wave's 64 pieces follow each other in LDS: the lane picks the piece that belongs there
+        const uint8_t* src = row + (h * kLanes + (ln ^ swizzle<kD>(item / kLanes % kKeys))) * 16;
+        typedef __attribute__((address_space(1))) const uint32_t global_u32;
+        typedef __attribute__((address_space(3))) uint32_t lds_u32;
+        __builtin_amdgcn_global_load_lds(
+            (global_u32*)(reinterpret_cast<uintptr_t>(src)),
+            (lds_u32*)(buf + (wave * 64 + x * kThreads) * 16), 16, 0, 0);
+      } else {
+        data[x] = *reinterpret_cast<const u32x4*>(row + (h * kLanes + ln) * 16);
+        if constexpr (kKind == 3) {
+          exponent[x] = row[a.num_kv_heads * (kD / 2) + h * (kD / 32) + ln];
+        }
       }
     }
   };
-  // the loaded rows as 16-bit values in LDS
-  auto stage = [&](int j, const int (&s)[kSl], bool look) {
-    uint8_t* buf = lds + (j & 1) * kBuf;
-    bool odd = false;
+  // what a step's rows still need before they can be read: the widened values, and where a row
+  // is past the list (V: zeros, K: anything) or outside the pool (V: zeros, K: NaN)
+  auto stage = [&](const int (&s)[kSl], lds_u8* buf) {
+    if constexpr (kDirect) {
+      __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): this wave's pieces are in LDS
+      int least = 0;
+#pragma unroll
+      for (int x = 0; x < kSl; ++x) least = min(least, s[x]);
+      if (__ballot(least < 0) == 0) return;
+    }
 #pragma unroll
     for (int x = 0; x < kLd; ++x) {
       const int item = tid + x * kThreads;
@@ -220,33 +250,28 @@ void prompt_kernel(PromptArgs a) {
       const int ln = item % kLanes;
       constexpr int kOut = kKind <= 1 ? 1 : kKind == 2 ? 2 : 4;   // 16-byte pieces of LDS
       u32x4 o[kOut];
-      if constexpr (kKind <= 1) {
-        o[0] = data[x];
-      } else if constexpr (kKind == 2) {
+      if constexpr (kKind == 2) {
         o[0] = widen_fp8<kBf16>(u32x2{data[x].x, data[x].y});
         o[1] = widen_fp8<kBf16>(u32x2{data[x].z, data[x].w});
-      } else {
+      } else if constexpr (kKind == 3) {
         const float e = e8m0_scale(exponent[x]);
 #pragma unroll
         for (int y = 0; y < 4; ++y) o[y] = widen_fp4(data[x][y], e);
       }
       const int slot = s[x % kSl];
-      if (slot < 0) {   // nothing of V; K of a slot outside the pool is NaN to whoever sees it
+      if (slot < 0) {
         const uint32_t fill = slot == -2 && !is_v ? 0x7fff7fffu : 0u;
 #pragma unroll
         for (int y = 0; y < kOut; ++y) o[y] = u32x4{fill, fill, fill, fill};
+      } else if (kDirect) {
+        continue;
       }
-      uint8_t* dst = is_v ? buf + kKeys * kRowK + row * kRowV : buf + row * kRowK;
+      lds_u8* dst = buf + (is_v ? kKeys * kRow : 0);
 #pragma unroll
       for (int y = 0; y < kOut; ++y) {
-        *reinterpret_cast<u32x4*>(dst + (ln * kOut + y) * 16) = o[y];
-        if (look && is_v) {
-#pragma unroll
-          for (int z = 0; z < 4; ++z) odd |= any_nonfinite<kBf16>(o[y][z]);
-        }
+        *(lds_u32x4*)(dst + piece_at<kD>(row, ln * kOut + y)) = o[y];
       }
     }
-    if (look && odd) nonfinite[j & 1] = j;
   };
   // whether every key of step j is seen by all of the rows of ranks [first, last]
   auto all_seen = [&](int j, int first, int lst) {
@@ -263,34 +288,41 @@ void prompt_kernel(PromptArgs a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[dc][e] = 0.f;
 
-  auto compute = [&](int j) {
-    const uint8_t* buf = lds + (j & 1) * kBuf;
+  // One step of the wave's rows; kFull: they see all of its keys
+  auto compute = [&](int j, const lds_u8* buf, auto full_t) {
+    constexpr bool kFull = decltype(full_t)::value;
+    // K piece 2 c + half of row lane & 31 is at at_k ^ 32 c; V piece 4 dc + vpiece of row vrow at
+    // at_v ^ 64 dc, of row vrow + 8 at (at_v ^ 64 dc ^ 32) + 8 rows: formed anew in each step (kept
+    // over the loop they would take two dozen registers)
+    uint32_t at_k = piece_at<kD>(lane & 31, half);
+    uint32_t at_v = piece_at<kD>(4 * half + (lane & 15) / 4,
+                                 (lane >> 4 & 1) * 2 + (lane >> 1 & 1)) + (lane & 1) * 8;
+    asm volatile("" : "+v"(at_k), "+v"(at_v));
     // ---- scores: lane holds keys 32 t + 8 (i / 4) + 4 half + i % 4 of its row
     f32x16 s[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
-      const uint8_t* src = buf + (32 * t + (lane & 31)) * kRowK + 16 * half;
 #pragma unroll
       for (int c = 0; c < kChunks; ++c) {
-        s[t] = mfma32<kBf16>(*reinterpret_cast<const u32x4*>(src + 32 * c), q[c], s[t]);
+        const lds_u8* src = buf + (at_k ^ (c << 5)) + 32 * t * kRow;
+        s[t] = mfma32<kBf16>(*(const lds_u32x4*)src, q[c], s[t]);
       }
     }
-    const bool full = all_seen(j, w_first, w_last);
     auto key_of = [&](int t, int e) {   // rank of the lane's key, or past every row's
       const int x = j * kKeys + 32 * t + 8 * (e / 4) + 4 * half + e % 4;
-      return x >= count ? INT32_MAX : x + (x < sk ? 0 : skip);
+      const int k = x + (x < sk ? 0 : skip);
+      return x >= count ? INT32_MAX : k;
     };
-    auto seen = [&](int k) {
-      return k <= p && (a.window == 0 || k > p - a.window || k < a.sinks);
-    };
-    if (!full) {
+    const int hidden = a.window > 0 ? p - a.window : INT32_MIN;   // the last key before the window
+    auto seen = [&](int k) { return (k <= p) & ((k > hidden) | (k < a.sinks)); };
+    if constexpr (!kFull) {
 #pragma unroll
       for (int t = 0; t < kTiles; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          if (!seen(key_of(t, e))) s[t][e] = -INFINITY;
+          s[t][e] = seen(key_of(t, e)) ? s[t][e] : -INFINITY;
         }
     }
     // ---- weights 2^(x - m); m follows the row's maximum where that passes it by 2^8 (the weights
@@ -321,8 +353,7 @@ void prompt_kernel(PromptArgs a) {
       }
     // ---- O^T += V^T . P^T, 16 keys at a time: a lane's weights 8 y .. 8 y + 7 of tile t are keys
     // 16 y + 4 half + (0..3) and those eight on; the V rows are read in that order
-    const uint8_t* vsrc = buf + kKeys * kRowK + (4 * half + (lane & 15) / 4) * kRowV +
-                          ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+    const lds_u8* vbuf = buf + kKeys * kRow;
     auto product = [&](auto clean) {
 #pragma unroll
       for (int t = 0; t < kTiles; ++t)
@@ -331,11 +362,13 @@ void prompt_kernel(PromptArgs a) {
           typename Act<kBf16>::x8 w;
 #pragma unroll
           for (int e = 0; e < 8; ++e) w[e] = static_cast<Elem>(s[t][8 * y + e]);
-          const uint8_t* src = vsrc + (32 * t + 16 * y) * kRowV;
+          const lds_u8* src = vbuf + (32 * t + 16 * y) * kRow;
 #pragma unroll
           for (int dc = 0; dc < kDC; ++dc) {
-            const i16x4 x1 = lds_read_tr16(src + dc * 64);
-            const i16x4 x2 = lds_read_tr16(src + 8 * kRowV + dc * 64);
+            const i16x4 x1 =
+                __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + (at_v ^ (dc << 6))));
+            const i16x4 x2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (lds_i16x4*)(src + (at_v ^ (dc << 6 | 32)) + 8 * kRow));
             const i16x8 xv = {x1[0], x1[1], x1[2], x1[3], x2[0], x2[1], x2[2], x2[3]};
             u32x4 v = __builtin_bit_cast(u32x4, xv);
             if constexpr (decltype(clean)::value) {
@@ -346,48 +379,77 @@ void prompt_kernel(PromptArgs a) {
           }
         }
     };
-    if (full || nonfinite[j & 1] != j) {
+    if constexpr (kFull) {
       product(std::false_type{});
     } else {
-      // a zero weight times an infinity would be NaN: the product goes without them, and the rows
-      // that see such a value take it as it is
-      product(std::true_type{});
-      for (int x = 0; x < kKeys; ++x) {
-        const int t = j * kKeys + x;
-        const int k = t >= count ? INT32_MAX : t + (t < sk ? 0 : skip);
-        const Elem* row = reinterpret_cast<const Elem*>(buf + kKeys * kRowK + x * kRowV);
-        const bool sees = seen(k);
+      // a zero weight times an infinity would be NaN: where V holds one, the product goes without
+      // it, and the rows that see such a value take it as it is
+      typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+      u16x2 most = {0, 0};
 #pragma unroll
-        for (int dc = 0; dc < kDC; ++dc)
+      for (int x = 0; x < kKeys * kRow; x += 1024) {
+        const u32x4 w = *(const lds_u32x4*)(vbuf + x + lane * 16);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float v = static_cast<float>(row[32 * dc + 8 * (e / 4) + 4 * half + e % 4]);
-            if (sees && !(fabsf(v) < INFINITY)) o[dc][e] += v;
-          }
+        for (int z = 0; z < 4; ++z) {
+          most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w[z] & 0x7fff7fffu));
+        }
+      }
+      constexpr uint16_t e = kBf16 ? 0x7f80 : 0x7c00;
+      if (__ballot(most.x >= e || most.y >= e) == 0) {
+        product(std::false_type{});
+      } else {
+        product(std::true_type{});
+        for (int x = 0; x < kKeys; ++x) {
+          const int t = j * kKeys + x;
+          const bool sees = seen(t >= count ? INT32_MAX : t + (t < sk ? 0 : skip));
+#pragma unroll
+          for (int dc = 0; dc < kDC; ++dc)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int d = 32 * dc + 8 * (e / 4) + 4 * half + e % 4;
+              typedef __attribute__((address_space(3))) const Elem lds_elem;
+              const float v = static_cast<float>(
+                  *(lds_elem*)(vbuf + piece_at<kD>(x, d / 8) + d % 8 * 2));
+              if (sees && !(fabsf(v) < INFINITY)) o[dc][e] += v;
+            }
+        }
       }
     }
   };
 
-  if (tid < 2) nonfinite[tid] = -1;
   int sa[kSl], sb[kSl];
-  if (step0 < step1) {
-    load_slots(step0, sa);
-    load_rows(sa);
-    load_slots(step0 + 1, sb);
-  }
-  __syncthreads();
-  for (int j = step0; j < step1; ++j) {
-    stage(j, sa, !all_seen(j, rank0 + i0, rank0 + last));
+  // Step j from `buf`, the next step's rows on their way to `other`. One barrier a step: `other`
+  // was last read in step j - 1, which every wave has left when it passes step j's barrier.
+  lds_u8* const buf0 = (lds_u8*)lds0;
+  lds_u8* const buf1 = (lds_u8*)lds1;
+  auto step = [&](int j, lds_u8* buf, lds_u8* other) {
+    stage(sa, buf);
+    if constexpr (!kDirect) {
+      if (j + 1 < step1) load_rows(sb, other);
+    }
+    __syncthreads();
     if (j + 1 < step1) {
+      if constexpr (kDirect) load_rows(sb, other);
 #pragma unroll
       for (int x = 0; x < kSl; ++x) sa[x] = sb[x];
-      load_rows(sa);
       load_slots(j + 2, sb);
     }
-    // one barrier a step: buffer j & 1 was last read two steps ago, before the last barrier
-    __syncthreads();
     const int k0 = j * kKeys + (j * kKeys < sk ? 0 : skip);
-    if (w_real && k0 <= w_last) compute(j);
+    if (!w_real || k0 > w_last) return;
+    if (all_seen(j, w_first, w_last)) {
+      compute(j, buf, std::true_type{});
+    } else {
+      compute(j, buf, std::false_type{});
+    }
+  };
+  if (step0 < step1) {
+    load_slots(step0, sa);
+    load_rows(sa, buf0);
+    load_slots(step0 + 1, sb);
+  }
+  for (int j = step0; j < step1; j += 2) {
+    step(j, buf0, buf1);
+    if (j + 1 < step1) step(j + 1, buf1, buf0);
   }
 
   // ---- the rows' results: lane holds values 32 dc + 8 (e / 4) + 4 half + e % 4
