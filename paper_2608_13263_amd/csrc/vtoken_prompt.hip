@@ -74,6 +74,18 @@ __device__ __forceinline__ Request find_request(const PromptArgs& a, int tau) {
   return f;
 }
 
+// A stored value (not of 4-bit rows).
+template <int kKind>
+__device__ __forceinline__ float element(const uint8_t* at) {
+  if constexpr (kKind == 0) {
+    return static_cast<float>(*reinterpret_cast<const _Float16*>(at));
+  } else if constexpr (kKind == 1) {
+    return static_cast<float>(*reinterpret_cast<const __bf16*>(at));
+  } else {
+    return __builtin_amdgcn_cvt_f32_fp8(*at, 0);
+  }
+}
+
 template <bool kBf16>
 __device__ __forceinline__ f32x16 mfma32(u32x4 x, u32x4 y, f32x16 acc) {
   if constexpr (kBf16) {
@@ -94,7 +106,7 @@ __device__ __forceinline__ float halves(float x) {
   return kMax ? fmaxf(a, b) : a + b;
 }
 
-// w with 16-bit halves that are infinities or NaN as zeros.
+// w with the 16-bit halves that are infinities or NaN as zeros.
 template <bool kBf16>
 __device__ __forceinline__ uint32_t only_finite(uint32_t w) {
   constexpr uint32_t e = kBf16 ? 0x7f80u : 0x7c00u;
@@ -138,6 +150,7 @@ void prompt_kernel(PromptArgs a) {
   // for the loads into the other
   __shared__ __attribute__((aligned(1024))) uint8_t lds0[2 * kKeys * kRow];
   __shared__ __attribute__((aligned(1024))) uint8_t lds1[2 * kKeys * kRow];
+  __shared__ int odd_step[2];   // the last step, by buffer, whose V had infinities or NaN
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -159,8 +172,6 @@ void prompt_kernel(PromptArgs a) {
   const int tok = m_row / G;
   const int last = min(i0 + tq, f.ql) - 1;            // last token of the tile
   const bool real = tok < tq && i0 + tok <= last;
-  const int64_t qrow = f.q0 + min(i0 + tok, last);
-  const int qh = h * G + m_row - tok * G;             // (of a row past the tile: any, not written)
   const int rank0 = n - f.ql;                         // rank of the request's query 0
   const int p = real ? rank0 + i0 + tok : -1;
   const int upper = max(rank0 + last + 1, 0);         // keys [0, upper) matter
@@ -179,8 +190,10 @@ void prompt_kernel(PromptArgs a) {
   // ---- the query operand: element e of chunk c is value 16 c + 8 half + e of the row
   u32x4 q[kChunks];
   {
-    const Elem* src = reinterpret_cast<const Elem*>(a.q) + qrow * a.q_stride +
-                      (int64_t)(real ? qh : h * G) * kD + 8 * half;
+    // (a row past the tile takes another's query; its results are not written)
+    const Elem* src = reinterpret_cast<const Elem*>(a.q) +
+                      (int64_t)(f.q0 + min(i0 + tok, last)) * a.q_stride +
+                      (int64_t)(h * G + (real ? m_row - tok * G : 0)) * kD + 8 * half;
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
       q[c] = *reinterpret_cast<const u32x4*>(src + 16 * c);
@@ -193,13 +206,20 @@ void prompt_kernel(PromptArgs a) {
 
   // ---- loads
   const uint8_t* kplane = a.kv + (int64_t)(2 * a.layer) * a.plane_bytes;
-  // slots of a step's rows: -1 past the list, -2 outside the pool
+  // slots of a step's rows
   auto load_slots = [&](int j, int (&s)[kSl]) {
 #pragma unroll
     for (int x = 0; x < kSl; ++x) {
       const int t = j * kKeys + (tid + x * kThreads) / kLanes % kKeys;
       const int k = t + (t < sk ? 0 : skip);
       s[x] = a.slots[(int64_t)s0 + (t < count ? k : 0)];
+    }
+  };
+  // -1 for those past the list, -2 outside the pool (once they have arrived)
+  auto mark_slots = [&](int j, int (&s)[kSl]) {
+#pragma unroll
+    for (int x = 0; x < kSl; ++x) {
+      const int t = j * kKeys + (tid + x * kThreads) / kLanes % kKeys;
       if (static_cast<unsigned>(s[x]) >= static_cast<unsigned>(a.num_slots)) s[x] = -2;
       if (t >= count) s[x] = -1;
     }
@@ -231,26 +251,34 @@ void prompt_kernel(PromptArgs a) {
       }
     }
   };
-  // what a step's rows still need before they can be read: the widened values, and where a row
-  // is past the list (V: zeros, K: anything) or outside the pool (V: zeros, K: NaN)
-  auto stage = [&](const int (&s)[kSl], lds_u8* buf) {
+  // What step j's rows still need before they can be read: the widened values; where a row is past
+  // the list (V: zeros, K: anything) or outside the pool (V: zeros, K: NaN); and where some row does
+  // not see all keys (`look`), zeros for V's infinities and NaN, since a zero weight times one of
+  // them would be NaN.
+  auto stage = [&](int j, const int (&s)[kSl], lds_u8* buf, bool look) {
     if constexpr (kDirect) {
       __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): this wave's pieces are in LDS
-      int least = 0;
-#pragma unroll
-      for (int x = 0; x < kSl; ++x) least = min(least, s[x]);
-      if (__ballot(least < 0) == 0) return;
+      if (!look) return;                    // (the list's end is a step of that kind)
     }
+    bool odd = false;
+    // piece y of item x is at (at ^ 16 y) + the rows of x items, formed anew in each step
+    constexpr int kOut = kKind <= 1 ? 1 : kKind == 2 ? 2 : 4;   // 16-byte pieces of LDS
+    constexpr int kPass = kThreads / kLanes;                    // rows of an item of every thread
+    static_assert(kDirect || kPass % 16 == 0, "the items' rows have one swizzle");
+    int thread = tid;
+    asm volatile("" : "+v"(thread));
+    const uint32_t at = piece_at<kD>(thread / kLanes % kKeys, thread % kLanes * kOut);
 #pragma unroll
     for (int x = 0; x < kLd; ++x) {
-      const int item = tid + x * kThreads;
+      const int item = thread + x * kThreads;
       if (2 * kItems < kThreads && item >= 2 * kItems) break;
-      const bool is_v = item >= kItems;
-      const int row = item / kLanes % kKeys;
-      const int ln = item % kLanes;
-      constexpr int kOut = kKind <= 1 ? 1 : kKind == 2 ? 2 : 4;   // 16-byte pieces of LDS
+      const bool is_v = kLd > 1 ? x >= kLd / 2 : item >= kItems;
+      lds_u8* dst = buf + (is_v ? kKeys * kRow : 0);
       u32x4 o[kOut];
-      if constexpr (kKind == 2) {
+      if constexpr (kDirect) {
+        dst += piece_at<kD>(item / kLanes % kKeys, item % kLanes ^ swizzle<kD>(item / kLanes % kKeys));
+        o[0] = *(lds_u32x4*)dst;
+      } else if constexpr (kKind == 2) {
         o[0] = widen_fp8<kBf16>(u32x2{data[x].x, data[x].y});
         o[1] = widen_fp8<kBf16>(u32x2{data[x].z, data[x].w});
       } else if constexpr (kKind == 3) {
@@ -263,15 +291,39 @@ void prompt_kernel(PromptArgs a) {
         const uint32_t fill = slot == -2 && !is_v ? 0x7fff7fffu : 0u;
 #pragma unroll
         for (int y = 0; y < kOut; ++y) o[y] = u32x4{fill, fill, fill, fill};
-      } else if (kDirect) {
-        continue;
       }
-      lds_u8* dst = buf + (is_v ? kKeys * kRow : 0);
+      if (kKind == 3 && look && is_v) {   // (the codes are finite)
+        if (exponent[kKind == 3 ? x : 0] == 255) {
+          odd |= slot >= 0;
+#pragma unroll
+          for (int y = 0; y < kOut; ++y) o[y] = u32x4{0, 0, 0, 0};
+        }
+      } else if (look && is_v) {
+#pragma unroll
+        for (int y = 0; y < kOut; ++y)
+#pragma unroll
+          for (int z = 0; z < 4; ++z) {
+            const uint32_t w = only_finite<kBf16>(o[y][z]);
+            odd |= w != o[y][z];
+            o[y][z] = w;
+          }
+      }
 #pragma unroll
       for (int y = 0; y < kOut; ++y) {
-        *(lds_u32x4*)(dst + piece_at<kD>(row, ln * kOut + y)) = o[y];
+        if constexpr (kDirect) {
+          *(lds_u32x4*)dst = o[y];
+        } else {
+          *(lds_u32x4*)(dst + (at ^ (y << 4)) + x % kSl * (kPass * kRow)) = o[y];
+        }
       }
     }
+    if (look && odd) odd_step[j & 1] = j;
+  };
+  auto any_outside = [&](const int (&s)[kSl]) {
+    int least = 0;
+#pragma unroll
+    for (int x = 0; x < kSl; ++x) least = min(least, s[x]);
+    return __ballot(least < -1) != 0;
   };
   // whether every key of step j is seen by all of the rows of ranks [first, last]
   auto all_seen = [&](int j, int first, int lst) {
@@ -281,6 +333,9 @@ void prompt_kernel(PromptArgs a) {
            (a.window == 0 || kmax < a.sinks || (t0 >= sk && kmin > lst - a.window));
   };
 
+  const int hidden = a.window > 0 ? p - a.window : INT32_MIN;   // the last key before the window
+  auto seen = [&](int k) { return (k <= p) & ((k > hidden) | (k < a.sinks)); };
+
   float m = -INFINITY, l = 0.f;
   f32x16 o[kDC];
 #pragma unroll
@@ -288,9 +343,8 @@ void prompt_kernel(PromptArgs a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[dc][e] = 0.f;
 
-  // One step of the wave's rows; kFull: they see all of its keys
-  auto compute = [&](int j, const lds_u8* buf, auto full_t) {
-    constexpr bool kFull = decltype(full_t)::value;
+  // One step of the wave's rows
+  auto compute = [&](int j, const lds_u8* buf) {
     // K piece 2 c + half of row lane & 31 is at at_k ^ 32 c; V piece 4 dc + vpiece of row vrow at
     // at_v ^ 64 dc, of row vrow + 8 at (at_v ^ 64 dc ^ 32) + 8 rows: formed anew in each step (kept
     // over the loop they would take two dozen registers)
@@ -315,9 +369,7 @@ void prompt_kernel(PromptArgs a) {
       const int k = x + (x < sk ? 0 : skip);
       return x >= count ? INT32_MAX : k;
     };
-    const int hidden = a.window > 0 ? p - a.window : INT32_MIN;   // the last key before the window
-    auto seen = [&](int k) { return (k <= p) & ((k > hidden) | (k < a.sinks)); };
-    if constexpr (!kFull) {
+    if (!all_seen(j, w_first, w_last)) {
 #pragma unroll
       for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -354,66 +406,49 @@ void prompt_kernel(PromptArgs a) {
     // ---- O^T += V^T . P^T, 16 keys at a time: a lane's weights 8 y .. 8 y + 7 of tile t are keys
     // 16 y + 4 half + (0..3) and those eight on; the V rows are read in that order
     const lds_u8* vbuf = buf + kKeys * kRow;
-    auto product = [&](auto clean) {
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t)
+    for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          typename Act<kBf16>::x8 w;
+      for (int y = 0; y < 2; ++y) {
+        typename Act<kBf16>::x8 w;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) w[e] = static_cast<Elem>(s[t][8 * y + e]);
-          const lds_u8* src = vbuf + (32 * t + 16 * y) * kRow;
+        for (int e = 0; e < 8; ++e) w[e] = static_cast<Elem>(s[t][8 * y + e]);
+        const lds_u8* src = vbuf + (32 * t + 16 * y) * kRow;
 #pragma unroll
-          for (int dc = 0; dc < kDC; ++dc) {
-            const i16x4 x1 =
-                __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + (at_v ^ (dc << 6))));
-            const i16x4 x2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds_i16x4*)(src + (at_v ^ (dc << 6 | 32)) + 8 * kRow));
-            const i16x8 xv = {x1[0], x1[1], x1[2], x1[3], x2[0], x2[1], x2[2], x2[3]};
-            u32x4 v = __builtin_bit_cast(u32x4, xv);
-            if constexpr (decltype(clean)::value) {
+        for (int dc = 0; dc < kDC; ++dc) {
+          const i16x4 x1 =
+              __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + (at_v ^ (dc << 6))));
+          const i16x4 x2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds_i16x4*)(src + (at_v ^ (dc << 6 | 32)) + 8 * kRow));
+          const i16x8 v = {x1[0], x1[1], x1[2], x1[3], x2[0], x2[1], x2[2], x2[3]};
+          o[dc] = mfma32<kBf16>(__builtin_bit_cast(u32x4, v), __builtin_bit_cast(u32x4, w), o[dc]);
+        }
+      }
+  };
+  // Step j's infinities and NaN of V, which LDS holds as zeros, for the rows that see them (from the
+  // cache: this is rare, and a row that sees one is lost anyway)
+  auto add_nonfinite = [&](int j) {
+#pragma unroll 1
+    for (int t = j * kKeys; t < min((j + 1) * kKeys, count); ++t) {
+      const int k = t + (t < sk ? 0 : skip);
+      const int slot = a.slots[(int64_t)s0 + k];
+      if (static_cast<unsigned>(slot) >= static_cast<unsigned>(a.num_slots) || !seen(k)) continue;
+      const uint8_t* row = kplane + a.plane_bytes + (int64_t)slot * a.row_bytes;
 #pragma unroll
-              for (int z = 0; z < 4; ++z) v[z] = only_finite<kBf16>(v[z]);
-            }
-            o[dc] = mfma32<kBf16>(v, __builtin_bit_cast(u32x4, w), o[dc]);
+      for (int dc = 0; dc < kDC; ++dc)
+        if constexpr (kKind == 3) {   // an exponent's 32 values are NaN, or none
+          if (row[a.num_kv_heads * (kD / 2) + h * (kD / 32) + dc] != 255) continue;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) o[dc][e] = __builtin_nanf("");
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const float v =
+                element<kKind>(row + (h * kD + 32 * dc + 8 * (e / 4) + 4 * half + e % 4) *
+                                         (kKind <= 1 ? 2 : 1));
+            if (!(fabsf(v) < INFINITY)) o[dc][e] += v;
           }
         }
-    };
-    if constexpr (kFull) {
-      product(std::false_type{});
-    } else {
-      // a zero weight times an infinity would be NaN: where V holds one, the product goes without
-      // it, and the rows that see such a value take it as it is
-      typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
-      u16x2 most = {0, 0};
-#pragma unroll
-      for (int x = 0; x < kKeys * kRow; x += 1024) {
-        const u32x4 w = *(const lds_u32x4*)(vbuf + x + lane * 16);
-#pragma unroll
-        for (int z = 0; z < 4; ++z) {
-          most = __builtin_elementwise_max(most, __builtin_bit_cast(u16x2, w[z] & 0x7fff7fffu));
-        }
-      }
-      constexpr uint16_t e = kBf16 ? 0x7f80 : 0x7c00;
-      if (__ballot(most.x >= e || most.y >= e) == 0) {
-        product(std::false_type{});
-      } else {
-        product(std::true_type{});
-        for (int x = 0; x < kKeys; ++x) {
-          const int t = j * kKeys + x;
-          const bool sees = seen(t >= count ? INT32_MAX : t + (t < sk ? 0 : skip));
-#pragma unroll
-          for (int dc = 0; dc < kDC; ++dc)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int d = 32 * dc + 8 * (e / 4) + 4 * half + e % 4;
-              typedef __attribute__((address_space(3))) const Elem lds_elem;
-              const float v = static_cast<float>(
-                  *(lds_elem*)(vbuf + piece_at<kD>(x, d / 8) + d % 8 * 2));
-              if (sees && !(fabsf(v) < INFINITY)) o[dc][e] += v;
-            }
-        }
-      }
     }
   };
 
@@ -423,37 +458,42 @@ void prompt_kernel(PromptArgs a) {
   lds_u8* const buf0 = (lds_u8*)lds0;
   lds_u8* const buf1 = (lds_u8*)lds1;
   auto step = [&](int j, lds_u8* buf, lds_u8* other) {
-    stage(sa, buf);
-    if constexpr (!kDirect) {
-      if (j + 1 < step1) load_rows(sb, other);
-    }
+    // (also where a slot may be outside the pool: those are looked for in every step)
+    const bool look = !all_seen(j, rank0 + i0, rank0 + last) || any_outside(sa);
+    stage(j, sa, buf, look);
+    const bool more = j + 1 < step1;
+    if (more) mark_slots(j + 1, sb);
+    if (!kDirect && more) load_rows(sb, other);
     __syncthreads();
-    if (j + 1 < step1) {
-      if constexpr (kDirect) load_rows(sb, other);
+    if (kDirect && more) load_rows(sb, other);
 #pragma unroll
-      for (int x = 0; x < kSl; ++x) sa[x] = sb[x];
-      load_slots(j + 2, sb);
-    }
+    for (int x = 0; x < kSl; ++x) sa[x] = sb[x];
+    if (j + 2 < step1) load_slots(j + 2, sb);
     const int k0 = j * kKeys + (j * kKeys < sk ? 0 : skip);
     if (!w_real || k0 > w_last) return;
-    if (all_seen(j, w_first, w_last)) {
-      compute(j, buf, std::true_type{});
-    } else {
-      compute(j, buf, std::false_type{});
-    }
+    compute(j, buf);
+    if (odd_step[j & 1] == j) add_nonfinite(j);
   };
+  if (tid < 2) odd_step[tid] = -1;
   if (step0 < step1) {
     load_slots(step0, sa);
+    mark_slots(step0, sa);
     load_rows(sa, buf0);
     load_slots(step0 + 1, sb);
   }
+  __syncthreads();   // odd_step
   for (int j = step0; j < step1; j += 2) {
     step(j, buf0, buf1);
     if (j + 1 < step1) step(j + 1, buf1, buf0);
   }
 
   // ---- the rows' results: lane holds values 32 dc + 8 (e / 4) + 4 half + e % 4
-  if (!real) return;
+  int at_row = m_row;   // (the row's place is worked out again, not kept over the loop)
+  asm volatile("" : "+v"(at_row));
+  const int tok2 = at_row / G;
+  if (tok2 >= tq || i0 + tok2 > last) return;
+  const int64_t qrow = f.q0 + i0 + tok2;
+  const int qh = h * G + at_row - tok2 * G;
   l = halves<false>(l);
   if (gridDim.y == 1) {
     const float inv = fixed ? __builtin_nanf("") : l == 0.f ? 0.f : 1.f / l;
