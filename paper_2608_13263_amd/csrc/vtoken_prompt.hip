@@ -354,16 +354,28 @@ void prompt_kernel(PromptArgs a) {
     asm volatile("" : "+v"(at_k), "+v"(at_v));
     // ---- scores: lane holds keys 32 t + 8 (i / 4) + 4 half + i % 4 of its row
     f32x16 s[kTiles];
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
+    for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) s[t][e] = 0.f;
 #pragma unroll
-      for (int c = 0; c < kChunks; ++c) {
+    for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
         const lds_u8* src = buf + (at_k ^ (c << 5)) + 32 * t * kRow;
         s[t] = mfma32<kBf16>(*(const lds_u32x4*)src, q[c], s[t]);
       }
+    // reads four products ahead
+    constexpr int kAhead = kChunks * kTiles < 4 ? kChunks * kTiles : 4;
+    __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+    for (int x = 0; x < kChunks * kTiles - kAhead; ++x) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
+    __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+    __builtin_amdgcn_s_setprio(0);
     auto key_of = [&](int t, int e) {   // rank of the lane's key, or past every row's
       const int x = j * kKeys + 32 * t + 8 * (e / 4) + 4 * half + e % 4;
       const int k = x + (x < sk ? 0 : skip);
@@ -396,34 +408,44 @@ void prompt_kernel(PromptArgs a) {
         for (int e = 0; e < 16; ++e) o[dc][e] *= by;
     }
     const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[t][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][e], scale, -base));
-        l += s[t][e];
-      }
     // ---- O^T += V^T . P^T, 16 keys at a time: a lane's weights 8 y .. 8 y + 7 of tile t are keys
-    // 16 y + 4 half + (0..3) and those eight on; the V rows are read in that order
+    // 16 y + 4 half + (0..3) and those eight on; the V rows are read in that order. The weights of
+    // the next 16 keys are formed while the matrix cores work on these.
     const lds_u8* vbuf = buf + kKeys * kRow;
+    constexpr int kGroups = 2 * kTiles;       // of 16 keys
+    constexpr int kPart = 8 / kDC > 0 ? 8 / kDC : 1;   // weights formed beside a product
+    auto weights = [&](typename Act<kBf16>::x8& w, int g, int e0, int n) {
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        typename Act<kBf16>::x8 w;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[e] = static_cast<Elem>(s[t][8 * y + e]);
-        const lds_u8* src = vbuf + (32 * t + 16 * y) * kRow;
-#pragma unroll
-        for (int dc = 0; dc < kDC; ++dc) {
-          const i16x4 x1 =
-              __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + (at_v ^ (dc << 6))));
-          const i16x4 x2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (lds_i16x4*)(src + (at_v ^ (dc << 6 | 32)) + 8 * kRow));
-          const i16x8 v = {x1[0], x1[1], x1[2], x1[3], x2[0], x2[1], x2[2], x2[3]};
-          o[dc] = mfma32<kBf16>(__builtin_bit_cast(u32x4, v), __builtin_bit_cast(u32x4, w), o[dc]);
-        }
+      for (int e = e0; e < e0 + n && e < 8; ++e) {
+        const float x = __builtin_amdgcn_exp2f(
+            __builtin_fmaf(s[g / 2][8 * (g % 2) + e], scale, -base));
+        l += x;
+        w[e] = static_cast<Elem>(x);
       }
+    };
+    auto v_operand = [&](int x) {   // of product x: group x / kDC, values 32 (x % kDC) ..
+      const lds_u8* src = vbuf + 16 * (x / kDC) * kRow;
+      const int dc = x % kDC;
+      const i16x4 x1 =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + (at_v ^ (dc << 6))));
+      const i16x4 x2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          (lds_i16x4*)(src + (at_v ^ (dc << 6 | 32)) + 8 * kRow));
+      const i16x8 v = {x1[0], x1[1], x1[2], x1[3], x2[0], x2[1], x2[2], x2[3]};
+      return __builtin_bit_cast(u32x4, v);
+    };
+    constexpr int kProducts = kGroups * kDC;
+    u32x4 v[3] = {v_operand(0), v_operand(1 < kProducts ? 1 : 0), {}};
+    typename Act<kBf16>::x8 w[2];
+    weights(w[0], 0, 0, 8);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int x = 0; x < kProducts; ++x) {
+      const int g = x / kDC, dc = x % kDC;
+      if (x + 2 < kProducts) v[(x + 2) % 3] = v_operand(x + 2);
+      o[dc] = mfma32<kBf16>(v[x % 3], __builtin_bit_cast(u32x4, w[g & 1]), o[dc]);
+      if (g + 1 < kGroups) weights(w[(g + 1) & 1], g + 1, dc * kPart, kPart);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
   // Step j's infinities and NaN of V, which LDS holds as zeros, for the rows that see them (from the
   // cache: this is rare, and a row that sees one is lost anyway)
