@@ -97,6 +97,19 @@ __device__ __forceinline__ f32x16 mfma32(u32x4 x, u32x4 y, f32x16 acc) {
   }
 }
 
+// sum + the two elements of pair i of w.
+template <bool kBf16>
+__device__ __forceinline__ float add_pair(const typename Act<kBf16>::x8& w, int i, float sum) {
+  typedef typename Act<kBf16>::x2 X2;
+  typedef typename Act<kBf16>::elem Elem;
+  const X2 x = {w[2 * i], w[2 * i + 1]}, one = {static_cast<Elem>(1.f), static_cast<Elem>(1.f)};
+  if constexpr (kBf16) {
+    return __builtin_amdgcn_fdot2_f32_bf16(x, one, sum, false);
+  } else {
+    return __builtin_amdgcn_fdot2(x, one, sum, false);
+  }
+}
+
 // x combined with the value of lane i ^ 32.
 template <bool kMax>
 __device__ __forceinline__ float halves(float x) {
@@ -205,45 +218,48 @@ void prompt_kernel(PromptArgs a) {
   const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504088896340736f;
 
   // ---- loads
+  const uint32_t num_slots = static_cast<uint32_t>(a.num_slots);
   const uint8_t* kplane = a.kv + (int64_t)(2 * a.layer) * a.plane_bytes;
-  // slots of a step's rows
-  auto load_slots = [&](int j, int (&s)[kSl]) {
+  // slots of a step's rows; those past the list re-read its last one
+  const int32_t* slots = a.slots + s0;
+  auto load_slots = [&](int j, uint32_t (&s)[kSl]) {
 #pragma unroll
     for (int x = 0; x < kSl; ++x) {
-      const int t = j * kKeys + (tid + x * kThreads) / kLanes % kKeys;
-      const int k = t + (t < sk ? 0 : skip);
-      s[x] = a.slots[(int64_t)s0 + (t < count ? k : 0)];
+      const int t = min(j * kKeys + (tid + x * kThreads) / kLanes % kKeys, count - 1);
+      s[x] = static_cast<uint32_t>(slots[t + (t < sk ? 0 : skip)]);
     }
   };
-  // -1 for those past the list, -2 outside the pool (once they have arrived)
-  auto mark_slots = [&](int j, int (&s)[kSl]) {
+  // whether one of them is outside the pool
+  auto any_outside = [&](const uint32_t (&s)[kSl]) {
+    uint32_t most = 0;
 #pragma unroll
-    for (int x = 0; x < kSl; ++x) {
-      const int t = j * kKeys + (tid + x * kThreads) / kLanes % kKeys;
-      if (static_cast<unsigned>(s[x]) >= static_cast<unsigned>(a.num_slots)) s[x] = -2;
-      if (t >= count) s[x] = -1;
-    }
+    for (int x = 0; x < kSl; ++x) most = max(most, s[x]);
+    return __ballot(most >= num_slots) != 0;
   };
   u32x4 data[kDirect ? 1 : kLd];
   uint32_t exponent[kKind == 3 ? kLd : 1];
-  auto load_rows = [&](const int (&s)[kSl], lds_u8* buf) {
+  const uint32_t row_bytes = static_cast<uint32_t>(a.row_bytes);
+  auto load_rows = [&](const uint32_t (&s)[kSl], lds_u8* buf) {
 #pragma unroll
     for (int x = 0; x < kLd; ++x) {
       const int item = tid + x * kThreads;
       if (2 * kItems < kThreads && item >= 2 * kItems) break;
-      const int slot = max(s[x % kSl], 0);
+      const bool is_v = kLd > 1 ? x >= kLd / 2 : item >= kItems;
+      const uint32_t slot = s[x % kSl] < num_slots ? s[x % kSl] : 0u;
       const int ln = item % kLanes;
-      const uint8_t* row =
-          kplane + (item / kItems) * a.plane_bytes + (int64_t)slot * a.row_bytes;
+      const uint8_t* plane = is_v ? kplane + a.plane_bytes : kplane;
       if constexpr (kDirect) {
         // a wave's 64 pieces follow each other in LDS: the lane picks the piece that belongs there
-        const uint8_t* src = row + (h * kLanes + (ln ^ swizzle<kD>(item / kLanes % kKeys))) * 16;
+        const uint8_t* src = plane +
+                             (h * kLanes + (ln ^ swizzle<kD>(item / kLanes % kKeys))) * 16 +
+                             (uint64_t)slot * row_bytes;
         typedef __attribute__((address_space(1))) const uint32_t global_u32;
         typedef __attribute__((address_space(3))) uint32_t lds_u32;
         __builtin_amdgcn_global_load_lds(
             (global_u32*)(reinterpret_cast<uintptr_t>(src)),
             (lds_u32*)(buf + (wave * 64 + x * kThreads) * 16), 16, 0, 0);
       } else {
+        const uint8_t* row = plane + (uint64_t)slot * row_bytes;
         data[x] = *reinterpret_cast<const u32x4*>(row + (h * kLanes + ln) * 16);
         if constexpr (kKind == 3) {
           exponent[x] = row[a.num_kv_heads * (kD / 2) + h * (kD / 32) + ln];
@@ -255,7 +271,7 @@ void prompt_kernel(PromptArgs a) {
   // the list (V: zeros, K: anything) or outside the pool (V: zeros, K: NaN); and where some row does
   // not see all keys (`look`), zeros for V's infinities and NaN, since a zero weight times one of
   // them would be NaN.
-  auto stage = [&](int j, const int (&s)[kSl], lds_u8* buf, bool look) {
+  auto stage = [&](int j, const uint32_t (&s)[kSl], lds_u8* buf, bool look) {
     if constexpr (kDirect) {
       __builtin_amdgcn_s_waitcnt(0x0f70);   // vmcnt(0): this wave's pieces are in LDS
       if (!look) return;                    // (the list's end is a step of that kind)
@@ -286,15 +302,17 @@ void prompt_kernel(PromptArgs a) {
 #pragma unroll
         for (int y = 0; y < 4; ++y) o[y] = widen_fp4(data[x][y], e);
       }
-      const int slot = s[x % kSl];
-      if (slot < 0) {
-        const uint32_t fill = slot == -2 && !is_v ? 0x7fff7fffu : 0u;
+      // (all of this is put right by every step that may need it, `look`)
+      const bool past = look && j * kKeys + item / kLanes % kKeys >= count;
+      const bool outside = look && s[x % kSl] >= num_slots;
+      if (past || outside) {
+        const uint32_t fill = past || is_v ? 0u : 0x7fff7fffu;
 #pragma unroll
         for (int y = 0; y < kOut; ++y) o[y] = u32x4{fill, fill, fill, fill};
       }
       if (kKind == 3 && look && is_v) {   // (the codes are finite)
         if (exponent[kKind == 3 ? x : 0] == 255) {
-          odd |= slot >= 0;
+          odd |= !past && !outside;
 #pragma unroll
           for (int y = 0; y < kOut; ++y) o[y] = u32x4{0, 0, 0, 0};
         }
@@ -318,12 +336,6 @@ void prompt_kernel(PromptArgs a) {
       }
     }
     if (look && odd) odd_step[j & 1] = j;
-  };
-  auto any_outside = [&](const int (&s)[kSl]) {
-    int least = 0;
-#pragma unroll
-    for (int x = 0; x < kSl; ++x) least = min(least, s[x]);
-    return __ballot(least < -1) != 0;
   };
   // whether every key of step j is seen by all of the rows of ranks [first, last]
   auto all_seen = [&](int j, int first, int lst) {
@@ -417,10 +429,10 @@ void prompt_kernel(PromptArgs a) {
     auto weights = [&](typename Act<kBf16>::x8& w, int g, int e0, int n) {
 #pragma unroll
       for (int e = e0; e < e0 + n && e < 8; ++e) {
-        const float x = __builtin_amdgcn_exp2f(
-            __builtin_fmaf(s[g / 2][8 * (g % 2) + e], scale, -base));
-        l += x;
-        w[e] = static_cast<Elem>(x);
+        w[e] = static_cast<Elem>(__builtin_amdgcn_exp2f(
+            __builtin_fmaf(s[g / 2][8 * (g % 2) + e], scale, -base)));
+        // the sum is that of the rounded weights, which the product takes
+        if (e % 2 == 1) l = add_pair<kBf16>(w, e / 2, l);
       }
     };
     auto v_operand = [&](int x) {   // of product x: group x / kDC, values 32 (x % kDC) ..
@@ -474,7 +486,7 @@ void prompt_kernel(PromptArgs a) {
     }
   };
 
-  int sa[kSl], sb[kSl];
+  uint32_t sa[kSl], sb[kSl];
   // Step j from `buf`, the next step's rows on their way to `other`. One barrier a step: `other`
   // was last read in step j - 1, which every wave has left when it passes step j's barrier.
   lds_u8* const buf0 = (lds_u8*)lds0;
@@ -484,7 +496,6 @@ void prompt_kernel(PromptArgs a) {
     const bool look = !all_seen(j, rank0 + i0, rank0 + last) || any_outside(sa);
     stage(j, sa, buf, look);
     const bool more = j + 1 < step1;
-    if (more) mark_slots(j + 1, sb);
     if (!kDirect && more) load_rows(sb, other);
     __syncthreads();
     if (kDirect && more) load_rows(sb, other);
@@ -499,7 +510,6 @@ void prompt_kernel(PromptArgs a) {
   if (tid < 2) odd_step[tid] = -1;
   if (step0 < step1) {
     load_slots(step0, sa);
-    mark_slots(step0, sa);
     load_rows(sa, buf0);
     load_slots(step0 + 1, sb);
   }
@@ -517,9 +527,14 @@ void prompt_kernel(PromptArgs a) {
   const int64_t qrow = f.q0 + i0 + tok2;
   const int qh = h * G + at_row - tok2 * G;
   l = halves<false>(l);
+  // what only the epilogue needs is read again, from the kernel's argument
+  auto* late = (const __attribute__((address_space(4))) PromptArgs*)
+      __builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(late));
   if (gridDim.y == 1) {
     const float inv = fixed ? __builtin_nanf("") : l == 0.f ? 0.f : 1.f / l;
-    Elem* dst = reinterpret_cast<Elem*>(a.out) + qrow * a.out_stride + (int64_t)qh * kD + 4 * half;
+    Elem* dst =
+        reinterpret_cast<Elem*>(late->out) + qrow * late->out_stride + (int64_t)qh * kD + 4 * half;
     typedef Elem Elem4 __attribute__((ext_vector_type(4)));
 #pragma unroll
     for (int dc = 0; dc < kDC; ++dc)
@@ -533,8 +548,8 @@ void prompt_kernel(PromptArgs a) {
       }
     return;
   }
-  float* rec = a.workspace +
-               ((qrow * a.num_kv_heads * G + qh) * gridDim.y + split) * (kD + 2);
+  float* rec = late->workspace +
+               ((qrow * late->num_kv_heads * G + qh) * gridDim.y + split) * (kD + 2);
   if (half == 0) {
     rec[0] = fixed ? __builtin_nanf("") : m;
     rec[1] = l;
