@@ -629,6 +629,9 @@ vtoken_status check_activation(const void* p, int64_t stride, int64_t width, int
   return VTOKEN_OK;
 }
 
+// Head rows (of q, k and v, over all tokens) that one call may have.
+constexpr int64_t kMaxHeadRows = 1LL << 27;
+
 int64_t plane_bytes_of(const vtoken_cache* c) {
   return (int64_t)c->num_blocks * c->block_size * c->num_kv_heads * c->head_dim * c->elem_bytes;
 }
@@ -654,10 +657,9 @@ vtoken_status vtoken_write_kv(const vtoken_cache* cache, const vtoken_kv_write* 
        w->rotary_dim % (w->interleaved != 0 ? 8 : 16) != 0)) {
     return VTOKEN_ERR_SHAPE;
   }
-  // a work item is a head row of a token; their number fits an int
-  const int64_t items =
-      w->num_tokens * ((int64_t)w->num_q_heads + 2 * (int64_t)w->num_kv_heads);
-  if (items > INT32_MAX) return VTOKEN_ERR_SHAPE;
+  // (32 lanes at most to a head row: thread indexes fit 32 bits)
+  const int64_t rows = (int64_t)w->num_q_heads + 2 * (int64_t)w->num_kv_heads;
+  if (rows > kMaxHeadRows / (w->num_tokens > 0 ? w->num_tokens : 1)) return VTOKEN_ERR_SHAPE;
   if (w->num_tokens == 0) return VTOKEN_OK;
   if (w->slots == nullptr || (w->cos_sin != nullptr && w->positions == nullptr)) {
     return VTOKEN_ERR_NULL;
@@ -697,6 +699,7 @@ vtoken_status vtoken_write_kv(const vtoken_cache* cache, const vtoken_kv_write* 
   a.interleaved = w->interleaved;
   a.num_slots = cache->num_blocks * cache->block_size;
   a.eps = w->eps;
+  a.inv_dim = 1. / D;
   return hip_status(
       vtoken::launch_write_kv(a, w->dtype == VTOKEN_KV_BF16, w->kv_dtype, stream));
 }
@@ -710,7 +713,7 @@ vtoken_status vtoken_read_kv(const vtoken_cache* cache, const vtoken_kv_read* r,
       VTOKEN_OK) {
     return s;
   }
-  if (r->num_tokens < 0 || 2 * (int64_t)r->num_kv_heads * r->num_tokens > INT32_MAX) {
+  if (r->num_tokens < 0 || 2 * (int64_t)r->num_kv_heads * r->num_tokens > kMaxHeadRows) {
     return VTOKEN_ERR_SHAPE;
   }
   if (r->num_tokens == 0) return VTOKEN_OK;

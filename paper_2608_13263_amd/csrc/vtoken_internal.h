@@ -403,6 +403,7 @@ struct WriteArgs {
   int32_t interleaved;
   int32_t num_slots;
   double eps;
+  double inv_dim;   // 1 / head_dim
 };
 struct ReadArgs {
   const int32_t* slots;

@@ -6,7 +6,9 @@
 //
 // A head row is taken by a group of lanes, eight elements (16 bytes) each, so that a group reads
 // its row with one load per lane, reduces and turns it in registers and stores it: every byte is
-// moved once. Both are bound by HBM where the calls are large and by latency where they are small.
+// moved once. A group takes kRowsPer rows of a token one after the other: their loads are in flight
+// together, and the angles, the weights and the token's slot and position are read once for them.
+// Both are bound by HBM where the calls are large and by latency where they are small.
 #include "vtoken_elements.h"
 
 namespace vtoken {
@@ -15,6 +17,64 @@ namespace {
 using namespace elements;
 
 constexpr int kRowThreads = 256;
+constexpr int kRowsPer = 4;
+
+// The value of another lane of the 16-lane row (DPP control word), without LDS.
+template <int kCtrl>
+__device__ __forceinline__ uint32_t dpp(uint32_t x) {
+  return static_cast<uint32_t>(
+      __builtin_amdgcn_update_dpp(0, static_cast<int>(x), kCtrl, 0xF, 0xF, false));
+}
+// Exchange with lane i ^ 1, i ^ 2, 3 - i of a quad, 7 - i of eight, 15 - i and (i + 8) % 16 of a row.
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kQuadMirror = 0x1B, kHalfMirror = 0x141, kMirror = 0x140,
+              kRor8 = 0x128;
+
+template <int kCtrl>
+__device__ __forceinline__ double dpp_add(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint64_t v = static_cast<uint64_t>(dpp<kCtrl>(static_cast<uint32_t>(u >> 32))) << 32 |
+                     dpp<kCtrl>(static_cast<uint32_t>(u));
+  return x + __builtin_bit_cast(double, v);
+}
+
+// Sum over a group of kLanes lanes (all of them active).
+template <int kLanes>
+__device__ __forceinline__ double group_sum(double x) {
+  x = dpp_add<kXor1>(x);
+  x = dpp_add<kXor2>(x);
+  if constexpr (kLanes >= 8) x = dpp_add<kHalfMirror>(x);
+  if constexpr (kLanes >= 16) x = dpp_add<kMirror>(x);
+  if constexpr (kLanes == 32) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = static_cast<uint32_t>(u), hi = static_cast<uint32_t>(u >> 32);
+    const auto l = __builtin_amdgcn_permlane16_swap(lo, lo, false, false);
+    const auto h = __builtin_amdgcn_permlane16_swap(hi, hi, false, false);
+    x = __builtin_bit_cast(double, static_cast<uint64_t>(h[0]) << 32 | l[0]) +
+        __builtin_bit_cast(double, static_cast<uint64_t>(h[1]) << 32 | l[1]);
+  }
+  return x;
+}
+
+// The value of the lane half a group on.
+template <int kLanes>
+__device__ __forceinline__ float other_half(float x) {
+  const uint32_t u = __float_as_uint(x);
+  if constexpr (kLanes == 4) return __uint_as_float(dpp<kXor2>(u));
+  if constexpr (kLanes == 8) return __uint_as_float(dpp<kQuadMirror>(dpp<kHalfMirror>(u)));
+  if constexpr (kLanes == 16) return __uint_as_float(dpp<kRor8>(u));
+  const auto r = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return __uint_as_float((threadIdx.x & 16) != 0 ? r[0] : r[1]);
+}
+
+// 1 / sqrt(v) to the last bits of a double (two Newton steps from the instruction's estimate; a
+// quarter of the time of a root and a division).
+__device__ __forceinline__ double inverse_root(double v) {
+  double y = __builtin_amdgcn_rsq(v);
+  if (y == 0.) return y;   // of an infinity
+#pragma unroll
+  for (int i = 0; i < 2; ++i) y = fma(0.5 * y, fma(-v * y, y, 1.), y);
+  return y;
+}
 
 template <bool kBf16>
 __device__ __forceinline__ void to_float(u32x4 w, float (&x)[8]) {
@@ -57,8 +117,8 @@ __device__ __forceinline__ void store_row(uint8_t* row, int heads, int head_dim,
     int top = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max(top, __float_as_int(x[i]) & 0x7fffffff);
-    top = max(top, __shfl_xor(top, 1, 64));
-    top = max(top, __shfl_xor(top, 2, 64));
+    top = max(top, static_cast<int>(dpp<kXor1>(top)));
+    top = max(top, static_cast<int>(dpp<kXor2>(top)));
     const int field = top >> 23;
     const int e = field == 255 ? 255 : max(field - 2, 1);
     const float inverse = e == 255 ? 0.f : __int_as_float((254 - e) << 23);
@@ -78,95 +138,140 @@ __device__ __forceinline__ void store_row(uint8_t* row, int heads, int head_dim,
   }
 }
 
+// Eight floats of a caller's buffer.
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+  const f32x4 a = *reinterpret_cast<const f32x4_in*>(p);
+  const f32x4 b = *reinterpret_cast<const f32x4_in*>(p + 4);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    x[j] = a[j];
+    x[4 + j] = b[j];
+  }
+}
+
 // kLanes: lanes per head row (the power of two from head_dim / 8 on, at least 4).
 template <int kLanes, bool kBf16, int kKind>
 __global__ __launch_bounds__(kRowThreads) void write_kernel(WriteArgs a) {
   // the results decide roundings to 8 and 4 bits: no contraction, the formula's own roundings
 #pragma clang fp contract(off)
-  const int items = a.num_q_heads + 2 * a.num_kv_heads;   // head rows of a token: q, k, v
-  const int64_t item = ((int64_t)blockIdx.x * kRowThreads + threadIdx.x) / kLanes;
+  const int rows = a.num_q_heads + 2 * a.num_kv_heads;   // head rows of a token: q, k, v
+  const uint32_t parts = (rows + kRowsPer - 1) / kRowsPer;
+  const uint32_t group = (blockIdx.x * kRowThreads + threadIdx.x) / kLanes;
   const int sub = threadIdx.x % kLanes;
-  if (item >= (int64_t)a.num_tokens * items) return;
-  const int t = static_cast<int>(item / items);
-  const int i = static_cast<int>(item) - t * items;
-  const int slot = a.slots[t];
-  if (slot < 0) return;
-  const bool is_q = i < a.num_q_heads;
-  const bool is_v = i >= a.num_q_heads + a.num_kv_heads;
-  const int h = is_q ? i : is_v ? i - a.num_q_heads - a.num_kv_heads : i - a.num_q_heads;
+  const uint32_t tok = group / parts;
+  const int row0 = static_cast<int>(group - tok * parts) * kRowsPer;
+  // (the lanes of a wave stay together: they exchange values)
+  const int t = min(tok, static_cast<uint32_t>(a.num_tokens - 1));
+  const int slot = tok < static_cast<uint32_t>(a.num_tokens) ? a.slots[t] : -1;
   const int D = a.head_dim;
   const int half = a.rotary_dim / 2;
-  const bool mine = sub * 8 < D;
+  const int e = sub * 8;
   const int pos = half > 0 ? a.positions[t] : 0;
   const bool bad = slot >= a.num_slots ||
                    (half > 0 && static_cast<unsigned>(pos) >= static_cast<unsigned>(a.num_positions));
-  if (bad && !is_q) return;
+  const bool mine = e < D && slot >= 0;
+  const int k0 = a.num_q_heads, v0 = k0 + a.num_kv_heads;
 
-  const uint8_t* src = is_q ? a.q : is_v ? a.v : a.k;
-  const int64_t stride = is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride;
-  float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (mine) {
-    to_float<kBf16>(*reinterpret_cast<const u32x4*>(src + (t * stride + h * D + sub * 8) * 2), x);
+  u32x4 raw[kRowsPer];
+#pragma unroll
+  for (int j = 0; j < kRowsPer; ++j) {
+    const int i = row0 + j;
+    const bool is_q = i < k0, is_v = i >= v0;
+    const uint8_t* src = is_q ? a.q : is_v ? a.v : a.k;
+    const int64_t stride = is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride;
+    const int h = is_q ? i : is_v ? i - v0 : i - k0;
+    raw[j] = u32x4{0, 0, 0, 0};
+    if (mine && i < rows) {
+      raw[j] = *reinterpret_cast<const u32x4*>(src + (t * stride + h * D + e) * 2);
+    }
   }
-  if (!is_v) {
-    const float* weight = is_q ? a.q_weight : a.k_weight;
-    if (weight != nullptr) {
+  // the angles of this lane's values: pairs (2 j, 2 j + 1), or values at and half / 8 lanes on
+  const bool turns = half > 0 && e < a.rotary_dim && row0 < v0;
+  float c[8] = {}, s[8] = {};
+  if (turns) {
+    const float* cs = a.cos_sin + (bad ? 0 : (int64_t)pos * a.rotary_dim);
+    if (a.interleaved) {
+      const f32x4 x = *reinterpret_cast<const f32x4_in*>(cs + e / 2);
+      const f32x4 y = *reinterpret_cast<const f32x4_in*>(cs + half + e / 2);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        c[j] = x[j];
+        s[j] = y[j];
+      }
+    } else {
+      const int at = e < half ? e : e - half;
+      load8(cs + at, c);
+      load8(cs + half + at, s);
+    }
+  }
+  float weight[8] = {};
+#pragma unroll
+  for (int j = 0; j < kRowsPer; ++j) {
+    const int i = row0 + j;
+    const bool is_q = i < k0, is_v = i >= v0;
+    const int h = is_q ? i : is_v ? i - v0 : i - k0;
+    float x[8];
+    to_float<kBf16>(raw[j], x);
+    const float* w = is_q ? a.q_weight : is_v ? nullptr : a.k_weight;
+    if (w != nullptr && (j == 0 || i == k0) && e < D) load8(w + e, weight);
+    if (row0 < v0 && (a.q_weight != nullptr || a.k_weight != nullptr)) {
       double sum = 0.;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum += static_cast<double>(x[j]) * x[j];
+      for (int y = 0; y < 8; ++y) {
+        const double z = x[y];
+        sum = fma(z, z, sum);
+      }
+      const float r =
+          static_cast<float>(inverse_root(group_sum<kLanes>(sum) * a.inv_dim + a.eps));
+      if (w != nullptr) {
 #pragma unroll
-      for (int d = 1; d < kLanes; d <<= 1) sum += __shfl_xor(sum, d, 64);
-      const float r = static_cast<float>(1. / sqrt(sum / D + a.eps));
-      if (mine) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = x[j] * r * weight[sub * 8 + j];
+        for (int y = 0; y < 8; ++y) x[y] = x[y] * r * weight[y];
       }
     }
-    if (half > 0) {
-      const float* cs = a.cos_sin + (bad ? 0 : (int64_t)pos * a.rotary_dim);
-      const int e = sub * 8;
+    if (half > 0 && row0 < v0) {
       if (a.interleaved) {
-        if (!bad && e < a.rotary_dim) {
+        if (turns && !is_v) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float c = cs[e / 2 + j], s = cs[half + e / 2 + j];
-            const float p = x[2 * j], q = x[2 * j + 1];
-            x[2 * j] = p * c - q * s;
-            x[2 * j + 1] = q * c + p * s;
+          for (int y = 0; y < 4; ++y) {
+            const float p = x[2 * y], q = x[2 * y + 1];
+            x[2 * y] = p * c[y] - q * s[y];
+            x[2 * y + 1] = q * c[y] + p * s[y];
           }
         }
       } else {
-        // the other half's values are half / 8 lanes on (or back)
-        const int d = half / 8;
-        const int from = (threadIdx.x & 63) + (e < half ? d : -d);
-        float y[8];
+        float o[8];
+        if (a.rotary_dim == kLanes * 8) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] = __shfl(x[j], from & 63, 64);
-        if (!bad && e < a.rotary_dim) {
-          const int at = e < half ? e : e - half;
+          for (int y = 0; y < 8; ++y) o[y] = other_half<kLanes>(x[y]);
+        } else {
+          const int from = (threadIdx.x & 63) + (e < half ? half / 8 : -(half / 8));
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const float c = cs[at + j], s = cs[half + at + j];
-            x[j] = e < half ? x[j] * c - y[j] * s : x[j] * c + y[j] * s;
+          for (int y = 0; y < 8; ++y) o[y] = __shfl(x[y], from & 63, 64);
+        }
+        if (turns && !is_v) {
+#pragma unroll
+          for (int y = 0; y < 8; ++y) {
+            const float p = x[y] * c[y], q = o[y] * s[y];
+            x[y] = e < half ? p - q : p + q;
           }
         }
       }
     }
-  }
-  if (!mine) return;
-  if (is_q) {
-    u32x4 w = to_act<kBf16>(x);
-    if (bad) {
-      float nan[8];
+    if (i >= rows) continue;
+    if (is_q) {
+      if (!mine) continue;
+      if (bad) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) nan[j] = __builtin_nanf("");
-      w = to_act<kBf16>(nan);
+        for (int y = 0; y < 8; ++y) x[y] = __builtin_nanf("");
+      }
+      *reinterpret_cast<u32x4*>(a.q_out + (t * a.q_out_stride + h * D + e) * 2) = to_act<kBf16>(x);
+      continue;
     }
-    *reinterpret_cast<u32x4*>(a.q_out + (t * a.q_out_stride + h * D + sub * 8) * 2) = w;
-    return;
+    if (mine && !bad) {
+      store_row<kBf16, kKind>((is_v ? a.vplane : a.kplane) + slot * a.row_bytes, a.num_kv_heads, D,
+                              h, sub, x);
+    }
   }
-  store_row<kBf16, kKind>((is_v ? a.vplane : a.kplane) + slot * a.row_bytes, a.num_kv_heads, D, h,
-                          sub, x);
 }
 
 // A lane's eight values of head h from a cache row, as activations.
@@ -186,27 +291,34 @@ __device__ __forceinline__ u32x4 load_row(const uint8_t* row, int heads, int hea
 
 template <int kLanes, bool kBf16, int kKind>
 __global__ __launch_bounds__(kRowThreads) void read_kernel(ReadArgs a) {
-  const int items = 2 * a.num_kv_heads;
-  const int64_t item = ((int64_t)blockIdx.x * kRowThreads + threadIdx.x) / kLanes;
+  const int rows = 2 * a.num_kv_heads;
+  const uint32_t parts = (rows + kRowsPer - 1) / kRowsPer;
+  const uint32_t group = (blockIdx.x * kRowThreads + threadIdx.x) / kLanes;
   const int sub = threadIdx.x % kLanes;
-  if (item >= (int64_t)a.num_tokens * items || sub * 8 >= a.head_dim) return;
-  const int t = static_cast<int>(item / items);
-  const int i = static_cast<int>(item) - t * items;
-  const bool is_v = i >= a.num_kv_heads;
-  const int h = is_v ? i - a.num_kv_heads : i;
+  const uint32_t tok = group / parts;
+  const int row0 = static_cast<int>(group - tok * parts) * kRowsPer;
+  if (tok >= static_cast<uint32_t>(a.num_tokens) || sub * 8 >= a.head_dim) return;
+  const int t = static_cast<int>(tok);
   const int slot = a.slots[t];
-  u32x4 w;
-  if (static_cast<unsigned>(slot) < static_cast<unsigned>(a.num_slots)) {
-    w = load_row<kBf16, kKind>((is_v ? a.vplane : a.kplane) + slot * a.row_bytes, a.num_kv_heads,
-                               a.head_dim, h, sub);
-  } else {
-    float nan[8];
+  const bool ok = static_cast<unsigned>(slot) < static_cast<unsigned>(a.num_slots);
+  u32x4 w[kRowsPer];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) nan[j] = __builtin_nanf("");
-    w = to_act<kBf16>(nan);
+  for (int j = 0; j < kRowsPer; ++j) {
+    const int i = row0 + j < rows ? row0 + j : row0;
+    const bool is_v = i >= a.num_kv_heads;
+    w[j] = load_row<kBf16, kKind>((is_v ? a.vplane : a.kplane) + (ok ? slot : 0) * a.row_bytes,
+                                  a.num_kv_heads, a.head_dim, is_v ? i - a.num_kv_heads : i, sub);
   }
-  *reinterpret_cast<u32x4*>((is_v ? a.v_out + t * a.v_stride * 2 : a.k_out + t * a.k_stride * 2) +
-                            (h * a.head_dim + sub * 8) * 2) = w;
+#pragma unroll
+  for (int j = 0; j < kRowsPer; ++j) {
+    const int i = row0 + j;
+    if (i >= rows) break;
+    const bool is_v = i >= a.num_kv_heads;
+    const int h = is_v ? i - a.num_kv_heads : i;
+    const u32x4 nan = {0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
+    uint8_t* dst = is_v ? a.v_out + t * a.v_stride * 2 : a.k_out + t * a.k_stride * 2;
+    *reinterpret_cast<u32x4*>(dst + (h * a.head_dim + sub * 8) * 2) = ok ? w[j] : nan;
+  }
 }
 
 int row_lanes(int head_dim) {
@@ -214,11 +326,12 @@ int row_lanes(int head_dim) {
 }
 
 template <template <int, bool, int> class Kernel, typename Args>
-hipError_t launch_rows(const Args& a, int64_t items, int head_dim, bool bf16, int kind,
-                       hipStream_t stream) {
+hipError_t launch_rows(const Args& a, int64_t tokens, int64_t rows, int head_dim, bool bf16,
+                       int kind, hipStream_t stream) {
   const int lanes = row_lanes(head_dim);
-  const int64_t groups = (items * lanes + kRowThreads - 1) / kRowThreads;
-  if (groups > INT32_MAX) return hipErrorInvalidValue;
+  const int64_t parts = (rows + kRowsPer - 1) / kRowsPer;
+  const int64_t groups = (tokens * parts * lanes + kRowThreads - 1) / kRowThreads;
+  if (groups * kRowThreads > UINT32_MAX) return hipErrorInvalidValue;   // (thread indexes)
   void (*kernel)(Args) = nullptr;
   auto pick = [&](auto lanes_t) {
     constexpr int kLanes = decltype(lanes_t)::value;
@@ -253,12 +366,12 @@ struct Read {
 }  // namespace
 
 hipError_t launch_write_kv(const WriteArgs& a, bool bf16, int kind, hipStream_t stream) {
-  return launch_rows<Write>(a, (int64_t)a.num_tokens * (a.num_q_heads + 2 * a.num_kv_heads),
+  return launch_rows<Write>(a, a.num_tokens, a.num_q_heads + 2 * (int64_t)a.num_kv_heads,
                             a.head_dim, bf16, kind, stream);
 }
 
 hipError_t launch_read_kv(const ReadArgs& a, bool bf16, int kind, hipStream_t stream) {
-  return launch_rows<Read>(a, (int64_t)a.num_tokens * 2 * a.num_kv_heads, a.head_dim, bf16, kind,
+  return launch_rows<Read>(a, a.num_tokens, 2 * (int64_t)a.num_kv_heads, a.head_dim, bf16, kind,
                            stream);
 }
 
