@@ -479,7 +479,7 @@ int64_t vtoken_kv_row_bytes(int32_t num_kv_heads, int32_t head_dim, int32_t kv_d
  * All in float32, rounded once (nearest even): to dtype for q, to the cache's type for k and v.
  * fp8 saturates at 448; 4 bits take per 32 values the exponent floor(log2(max |y|)) - 2, at least
  * 2^-126, and saturate at 6 (an infinity or NaN makes the 32 values NaN).
- * A negative slot marks padding: nothing of that token is read or written. A slot past the pool,
+ * A negative slot marks padding: nothing of that token is written. A slot past the pool,
  * or a position outside [0, num_positions) where there is a table, writes nothing to the cache and
  * NaN to the token's q_out. Slots of a call must differ (of two tokens with one slot, which values
  * stay is not defined). A call may have 2^27 head rows of q, k and v over all tokens (more:

@@ -149,44 +149,65 @@ __device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
   }
 }
 
-// kLanes: lanes per head row (the power of two from head_dim / 8 on, at least 4).
+// kLanes: lanes per head row (the power of two from head_dim / 8 on, at least 4). A group's rows are
+// all queries, all keys or all values.
 template <int kLanes, bool kBf16, int kKind>
 __global__ __launch_bounds__(kRowThreads) void write_kernel(WriteArgs a) {
   // the results decide roundings to 8 and 4 bits: no contraction, the formula's own roundings
 #pragma clang fp contract(off)
-  const int rows = a.num_q_heads + 2 * a.num_kv_heads;   // head rows of a token: q, k, v
-  const uint32_t parts = (rows + kRowsPer - 1) / kRowsPer;
-  const uint32_t group = (blockIdx.x * kRowThreads + threadIdx.x) / kLanes;
-  const int sub = threadIdx.x % kLanes;
-  const uint32_t tok = group / parts;
-  const int row0 = static_cast<int>(group - tok * parts) * kRowsPer;
-  // (the lanes of a wave stay together: they exchange values)
-  const int t = min(tok, static_cast<uint32_t>(a.num_tokens - 1));
-  const int slot = tok < static_cast<uint32_t>(a.num_tokens) ? a.slots[t] : -1;
   const int D = a.head_dim;
-  const int half = a.rotary_dim / 2;
+  const uint32_t q_parts = (a.num_q_heads + kRowsPer - 1) / kRowsPer;
+  const uint32_t kv_parts = (a.num_kv_heads + kRowsPer - 1) / kRowsPer;
+  const uint32_t parts = q_parts + 2 * kv_parts;
+  const uint32_t group = (blockIdx.x * kRowThreads + threadIdx.x) / kLanes;
+  const uint32_t tok = group / parts;
+  if (tok >= static_cast<uint32_t>(a.num_tokens)) return;   // (whole groups: they exchange values)
+  const uint32_t part = group - tok * parts;
+  const bool is_q = part < q_parts, is_v = part >= q_parts + kv_parts;
+  const uint32_t in_kind = part - (is_q ? 0u : is_v ? q_parts + kv_parts : q_parts);
+  const int h0 = static_cast<int>(in_kind) * kRowsPer;
+  const int n = min(kRowsPer, (is_q ? a.num_q_heads : a.num_kv_heads) - h0);   // rows of the group
+  const int64_t t = tok;
+  const int slot = a.slots[t];
+  const int sub = threadIdx.x % kLanes;
   const int e = sub * 8;
-  const int pos = half > 0 ? a.positions[t] : 0;
-  const bool bad = slot >= a.num_slots ||
-                   (half > 0 && static_cast<unsigned>(pos) >= static_cast<unsigned>(a.num_positions));
-  const bool mine = e < D && slot >= 0;
-  const int k0 = a.num_q_heads, v0 = k0 + a.num_kv_heads;
+  const bool full = D == kLanes * 8;      // (uniform) no lane is past the row
+  const bool mine = full || e < D;
 
+  const uint8_t* src = (is_q ? a.q : is_v ? a.v : a.k) +
+                       (t * (is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride) +
+                        (int64_t)h0 * D + (mine ? e : 0)) * 2;
   u32x4 raw[kRowsPer];
 #pragma unroll
   for (int j = 0; j < kRowsPer; ++j) {
-    const int i = row0 + j;
-    const bool is_q = i < k0, is_v = i >= v0;
-    const uint8_t* src = is_q ? a.q : is_v ? a.v : a.k;
-    const int64_t stride = is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride;
-    const int h = is_q ? i : is_v ? i - v0 : i - k0;
-    raw[j] = u32x4{0, 0, 0, 0};
-    if (mine && i < rows) {
-      raw[j] = *reinterpret_cast<const u32x4*>(src + (t * stride + h * D + e) * 2);
-    }
+    raw[j] = *reinterpret_cast<const u32x4*>(src + min(j, n - 1) * (D * 2));
   }
+  if (slot < 0) return;
+  const int half = a.rotary_dim / 2;
+  int pos = 0;
+  if (half > 0) pos = a.positions[t];
+  const bool bad =
+      slot >= a.num_slots ||
+      (half > 0 && static_cast<uint32_t>(pos) >= static_cast<uint32_t>(a.num_positions));
+  uint8_t* row = (is_v ? a.vplane : a.kplane) + (bad ? 0 : slot) * a.row_bytes;
+  if (is_v) {
+    if (bad || !mine) return;
+#pragma unroll
+    for (int j = 0; j < kRowsPer; ++j) {
+      if (j >= n) break;
+      if constexpr (kKind <= 1) {
+        *reinterpret_cast<u32x4*>(row + ((h0 + j) * D + e) * 2) = raw[j];
+      } else {
+        float x[8];
+        to_float<kBf16>(raw[j], x);
+        store_row<kBf16, kKind>(row, a.num_kv_heads, D, h0 + j, sub, x);
+      }
+    }
+    return;
+  }
+
   // the angles of this lane's values: pairs (2 j, 2 j + 1), or values at and half / 8 lanes on
-  const bool turns = half > 0 && e < a.rotary_dim && row0 < v0;
+  const bool turns = e < a.rotary_dim;
   float c[8] = {}, s[8] = {};
   if (turns) {
     const float* cs = a.cos_sin + (bad ? 0 : (int64_t)pos * a.rotary_dim);
@@ -203,34 +224,40 @@ __global__ __launch_bounds__(kRowThreads) void write_kernel(WriteArgs a) {
       load8(cs + at, c);
       load8(cs + half + at, s);
     }
+    // (a, b) -> (a c - b s, b c + a s): the first half's sines with their sign changed
+    if (!a.interleaved && e < half) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] = -s[j];
+    }
   }
+  const float* w = is_q ? a.q_weight : a.k_weight;
   float weight[8] = {};
+  if (w != nullptr && mine) load8(w + e, weight);
+  if (bad) {   // (queries: NaN; nothing of keys is stored)
+#pragma unroll
+    for (int j = 0; j < kRowsPer; ++j) raw[j] = u32x4{0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
+  }
+  uint8_t* out = is_q ? a.q_out + (t * a.q_out_stride + (int64_t)h0 * D + e) * 2 : nullptr;
 #pragma unroll
   for (int j = 0; j < kRowsPer; ++j) {
-    const int i = row0 + j;
-    const bool is_q = i < k0, is_v = i >= v0;
-    const int h = is_q ? i : is_v ? i - v0 : i - k0;
     float x[8];
     to_float<kBf16>(raw[j], x);
-    const float* w = is_q ? a.q_weight : is_v ? nullptr : a.k_weight;
-    if (w != nullptr && (j == 0 || i == k0) && e < D) load8(w + e, weight);
-    if (row0 < v0 && (a.q_weight != nullptr || a.k_weight != nullptr)) {
+    if (w != nullptr) {
       double sum = 0.;
 #pragma unroll
       for (int y = 0; y < 8; ++y) {
         const double z = x[y];
         sum = fma(z, z, sum);
       }
+      if (!mine) sum = 0.;
       const float r =
           static_cast<float>(inverse_root(group_sum<kLanes>(sum) * a.inv_dim + a.eps));
-      if (w != nullptr) {
 #pragma unroll
-        for (int y = 0; y < 8; ++y) x[y] = x[y] * r * weight[y];
-      }
+      for (int y = 0; y < 8; ++y) x[y] = x[y] * r * weight[y];
     }
-    if (half > 0 && row0 < v0) {
+    if (half > 0) {
       if (a.interleaved) {
-        if (turns && !is_v) {
+        if (turns) {
 #pragma unroll
           for (int y = 0; y < 4; ++y) {
             const float p = x[2 * y], q = x[2 * y + 1];
@@ -238,38 +265,27 @@ __global__ __launch_bounds__(kRowThreads) void write_kernel(WriteArgs a) {
             x[2 * y + 1] = q * c[y] + p * s[y];
           }
         }
+      } else if (a.rotary_dim == kLanes * 8) {
+#pragma unroll
+        for (int y = 0; y < 8; ++y) {
+          const float o = other_half<kLanes>(x[y]);
+          x[y] = x[y] * c[y] + o * s[y];
+        }
       } else {
-        float o[8];
-        if (a.rotary_dim == kLanes * 8) {
+        const int from = (threadIdx.x & 63) + (e < half ? half / 8 : -(half / 8));
 #pragma unroll
-          for (int y = 0; y < 8; ++y) o[y] = other_half<kLanes>(x[y]);
-        } else {
-          const int from = (threadIdx.x & 63) + (e < half ? half / 8 : -(half / 8));
-#pragma unroll
-          for (int y = 0; y < 8; ++y) o[y] = __shfl(x[y], from & 63, 64);
-        }
-        if (turns && !is_v) {
-#pragma unroll
-          for (int y = 0; y < 8; ++y) {
-            const float p = x[y] * c[y], q = o[y] * s[y];
-            x[y] = e < half ? p - q : p + q;
-          }
+        for (int y = 0; y < 8; ++y) {
+          const float o = __shfl(x[y], from & 63, 64);
+          const float z = x[y] * c[y] + o * s[y];
+          x[y] = turns ? z : x[y];
         }
       }
     }
-    if (i >= rows) continue;
+    if (j >= n || !mine) continue;
     if (is_q) {
-      if (!mine) continue;
-      if (bad) {
-#pragma unroll
-        for (int y = 0; y < 8; ++y) x[y] = __builtin_nanf("");
-      }
-      *reinterpret_cast<u32x4*>(a.q_out + (t * a.q_out_stride + h * D + e) * 2) = to_act<kBf16>(x);
-      continue;
-    }
-    if (mine && !bad) {
-      store_row<kBf16, kKind>((is_v ? a.vplane : a.kplane) + slot * a.row_bytes, a.num_kv_heads, D,
-                              h, sub, x);
+      *reinterpret_cast<u32x4*>(out + j * (D * 2)) = to_act<kBf16>(x);
+    } else if (!bad) {
+      store_row<kBf16, kKind>(row, a.num_kv_heads, D, h0 + j, sub, x);
     }
   }
 }
@@ -291,33 +307,31 @@ __device__ __forceinline__ u32x4 load_row(const uint8_t* row, int heads, int hea
 
 template <int kLanes, bool kBf16, int kKind>
 __global__ __launch_bounds__(kRowThreads) void read_kernel(ReadArgs a) {
-  const int rows = 2 * a.num_kv_heads;
-  const uint32_t parts = (rows + kRowsPer - 1) / kRowsPer;
+  const uint32_t kv_parts = (a.num_kv_heads + kRowsPer - 1) / kRowsPer;
   const uint32_t group = (blockIdx.x * kRowThreads + threadIdx.x) / kLanes;
   const int sub = threadIdx.x % kLanes;
-  const uint32_t tok = group / parts;
-  const int row0 = static_cast<int>(group - tok * parts) * kRowsPer;
+  const uint32_t tok = group / (2 * kv_parts);
   if (tok >= static_cast<uint32_t>(a.num_tokens) || sub * 8 >= a.head_dim) return;
-  const int t = static_cast<int>(tok);
+  const uint32_t part = group - tok * 2 * kv_parts;
+  const bool is_v = part >= kv_parts;
+  const int h0 = static_cast<int>(is_v ? part - kv_parts : part) * kRowsPer;
+  const int n = min(kRowsPer, a.num_kv_heads - h0);
+  const int64_t t = tok;
   const int slot = a.slots[t];
   const bool ok = static_cast<unsigned>(slot) < static_cast<unsigned>(a.num_slots);
+  const uint8_t* row = (is_v ? a.vplane : a.kplane) + (ok ? slot : 0) * a.row_bytes;
   u32x4 w[kRowsPer];
 #pragma unroll
   for (int j = 0; j < kRowsPer; ++j) {
-    const int i = row0 + j < rows ? row0 + j : row0;
-    const bool is_v = i >= a.num_kv_heads;
-    w[j] = load_row<kBf16, kKind>((is_v ? a.vplane : a.kplane) + (ok ? slot : 0) * a.row_bytes,
-                                  a.num_kv_heads, a.head_dim, is_v ? i - a.num_kv_heads : i, sub);
+    w[j] = load_row<kBf16, kKind>(row, a.num_kv_heads, a.head_dim, h0 + min(j, n - 1), sub);
   }
+  uint8_t* out = (is_v ? a.v_out + t * a.v_stride * 2 : a.k_out + t * a.k_stride * 2) +
+                 ((int64_t)h0 * a.head_dim + sub * 8) * 2;
 #pragma unroll
   for (int j = 0; j < kRowsPer; ++j) {
-    const int i = row0 + j;
-    if (i >= rows) break;
-    const bool is_v = i >= a.num_kv_heads;
-    const int h = is_v ? i - a.num_kv_heads : i;
+    if (j >= n) break;
     const u32x4 nan = {0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu, 0x7fff7fffu};
-    uint8_t* dst = is_v ? a.v_out + t * a.v_stride * 2 : a.k_out + t * a.k_stride * 2;
-    *reinterpret_cast<u32x4*>(dst + (h * a.head_dim + sub * 8) * 2) = ok ? w[j] : nan;
+    *reinterpret_cast<u32x4*>(out + j * (a.head_dim * 2)) = ok ? w[j] : nan;
   }
 }
 
@@ -325,11 +339,13 @@ int row_lanes(int head_dim) {
   return head_dim <= 32 ? 4 : head_dim <= 64 ? 8 : head_dim <= 128 ? 16 : 32;
 }
 
+// Groups of a token's heads of one kind.
+int64_t parts_of(int64_t heads) { return (heads + kRowsPer - 1) / kRowsPer; }
+
 template <template <int, bool, int> class Kernel, typename Args>
-hipError_t launch_rows(const Args& a, int64_t tokens, int64_t rows, int head_dim, bool bf16,
+hipError_t launch_rows(const Args& a, int64_t tokens, int64_t parts, int head_dim, bool bf16,
                        int kind, hipStream_t stream) {
   const int lanes = row_lanes(head_dim);
-  const int64_t parts = (rows + kRowsPer - 1) / kRowsPer;
   const int64_t groups = (tokens * parts * lanes + kRowThreads - 1) / kRowThreads;
   if (groups * kRowThreads > UINT32_MAX) return hipErrorInvalidValue;   // (thread indexes)
   void (*kernel)(Args) = nullptr;
@@ -366,12 +382,12 @@ struct Read {
 }  // namespace
 
 hipError_t launch_write_kv(const WriteArgs& a, bool bf16, int kind, hipStream_t stream) {
-  return launch_rows<Write>(a, a.num_tokens, a.num_q_heads + 2 * (int64_t)a.num_kv_heads,
+  return launch_rows<Write>(a, a.num_tokens, parts_of(a.num_q_heads) + 2 * parts_of(a.num_kv_heads),
                             a.head_dim, bf16, kind, stream);
 }
 
 hipError_t launch_read_kv(const ReadArgs& a, bool bf16, int kind, hipStream_t stream) {
-  return launch_rows<Read>(a, a.num_tokens, 2 * (int64_t)a.num_kv_heads, a.head_dim, bf16, kind,
+  return launch_rows<Read>(a, a.num_tokens, 2 * parts_of(a.num_kv_heads), a.head_dim, bf16, kind,
                            stream);
 }
 
