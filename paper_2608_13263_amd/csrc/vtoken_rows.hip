@@ -121,16 +121,14 @@ __device__ __forceinline__ void store_row(uint8_t* row, int heads, int head_dim,
     top = max(top, static_cast<int>(dpp<kXor2>(top)));
     const int field = top >> 23;
     const int e = field == 255 ? 255 : max(field - 2, 1);
-    const float inverse = e == 255 ? 0.f : __int_as_float((254 - e) << 23);
+    // x / 2^(e - 127) to the nearest code, ties to even ones, 6 at most
+    const float scale = __int_as_float(min(e, 254) << 23);
     uint32_t w = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float t = fabsf(x[i]) * inverse;   // exact but for what rounds to zero anyway
-      const uint32_t code = (t > 0.25f) + (t >= 0.75f) + (t > 1.25f) + (t >= 1.75f) +
-                            (t > 2.5f) + (t >= 3.5f) + (t > 5.f);
-      const uint32_t sign = e != 255 && __float_as_int(x[i]) < 0 ? 8u : 0u;
-      w |= (code | sign) << (4 * i);
-    }
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[0], x[1], scale, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[2], x[3], scale, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[4], x[5], scale, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, x[6], x[7], scale, 3);
+    if (e == 255) w = 0;
     *reinterpret_cast<uint32_t*>(row + h * (head_dim / 2) + sub * 4) = w;
     if ((sub & 3) == 0) {
       row[heads * (head_dim / 2) + h * (head_dim / 32) + sub / 4] = static_cast<uint8_t>(e);
