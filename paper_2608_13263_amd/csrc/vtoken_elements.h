@@ -74,12 +74,59 @@ __device__ __forceinline__ u32x4 widen_fp4(uint32_t w, float scale) {
   return o;
 }
 
+// LDS addresses, 32 bits wide.
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
+typedef __attribute__((address_space(3))) uint32_t lds_u32;
+
+// Rows of 16-bit values lie in LDS without padding (loads that write it directly leave none), 16-byte
+// piece c of row r at c ^ swizzle(r): the 16-byte reads of 16 rows at one c, and transpose reads of
+// 4 rows x 64 bytes or 8 rows x 32 bytes, then fall on different banks.
+template <int kD>
+__device__ __forceinline__ int swizzle(int r) {
+  const int low = (r >> 1 & 2) | (r >> 3 & 1);
+  return kD >= 128 ? (r & 3) << 2 | low : kD == 64 ? (r >> 1 & 1) << 2 | low : low;
+}
+template <int kD>
+__device__ __forceinline__ int piece_at(int r, int c) {   // byte offset
+  return r * (kD * 2) + ((c ^ swizzle<kD>(r)) << 4);
+}
+
+// A lane's 16 loaded bytes of fp8 or codes become 2 or 4 pieces of such a row. Written in order the
+// pieces of 16 neighbouring lanes would meet on the same banks: lane `ln` of row r writes piece
+// y ^ write_turn(r, ln) y-th.
+template <int kKind, int kD>
+__device__ __forceinline__ int write_turn(int r, int ln) {
+  if constexpr (kKind == 3) {
+    return kD == 256 ? (ln >> 2 & 1) | (r & 1) << 1 : kD == 128 ? r & 3 : kD == 64 ? r >> 1 & 1 : 0;
+  } else {
+    return kD == 256 ? ln >> 3 & 1 : kD == 128 ? r & 1 : kD == 64 ? r >> 1 & 1 : r >> 2 & 1;
+  }
+}
+
+// The pieces of 16 bytes of a cache row in the order in which they are written.
+template <bool kBf16, int kKind>
+__device__ __forceinline__ void widen(u32x4 w, float scale, int turn, u32x4* o) {
+  if constexpr (kKind == 3) {
+    const bool one = (turn & 1) != 0, two = (turn & 2) != 0;
+    const u32x4 x = {one ? w.y : w.x, one ? w.x : w.y, one ? w.w : w.z, one ? w.z : w.w};
+    o[0] = widen_fp4(two ? x.z : x.x, scale);
+    o[1] = widen_fp4(two ? x.w : x.y, scale);
+    o[2] = widen_fp4(two ? x.x : x.z, scale);
+    o[3] = widen_fp4(two ? x.y : x.w, scale);
+  } else {
+    const bool one = turn != 0;
+    o[0] = widen_fp8<kBf16>(one ? u32x2{w.z, w.w} : u32x2{w.x, w.y});
+    o[1] = widen_fp8<kBf16>(one ? u32x2{w.x, w.y} : u32x2{w.z, w.w});
+  }
+}
+
 // LDS transpose read (ds_read_b64_tr_b16): in each group of 16 lanes, lane 4a + b receives element
 // b of the four 16-bit values addressed by lanes a, a+4, a+8 and a+12 of its group.
-__device__ __forceinline__ i16x4 lds_read_tr16(const uint8_t* lds_addr) {
-  typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-      (lds_i16x4*)(reinterpret_cast<uintptr_t>(lds_addr)));
+__device__ __forceinline__ i16x4 lds_read_tr16(const lds_u8* at) {
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)at);
 }
 
 }  // namespace elements

@@ -17,10 +17,6 @@ namespace {
 using namespace elements;
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
-// LDS addresses, 32 bits wide
-typedef __attribute__((address_space(3))) uint8_t lds_u8;
-typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
-typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 
 constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
@@ -126,20 +122,6 @@ __device__ __forceinline__ uint32_t only_finite(uint32_t w) {
   if ((w & e) == e) w &= 0xffff0000u;
   if ((w & e << 16) == e << 16) w &= 0xffffu;
   return w;
-}
-
-// K and V rows lie in LDS without padding (the loads that write it directly leave none), 16-byte
-// piece c of row r at c ^ swizzle(r): the 16-byte reads of 16 rows at one c, and the transpose
-// reads of 4 rows x 64 bytes, then fall on different banks.
-template <int kD>
-__device__ __forceinline__ int swizzle(int r) {
-  if constexpr (kD >= 128) return (r & 3) << 2 | (r >> 2 & 3);
-  if constexpr (kD == 64) return (r >> 1 & 1) << 2 | (r >> 2 & 3);
-  return r >> 2 & 3;
-}
-template <int kD>
-__device__ __forceinline__ int piece_at(int r, int c) {   // byte offset
-  return r * (kD * 2) + ((c ^ swizzle<kD>(r)) << 4);
 }
 
 template <bool kBf16, int kKind, int kD>
@@ -283,7 +265,8 @@ void prompt_kernel(PromptArgs a) {
     static_assert(kDirect || kPass % 16 == 0, "the items' rows have one swizzle");
     int thread = tid;
     asm volatile("" : "+v"(thread));
-    const uint32_t at = piece_at<kD>(thread / kLanes % kKeys, thread % kLanes * kOut);
+    const int turn = write_turn<kKind, kD>(thread / kLanes % kKeys, thread % kLanes);
+    const uint32_t at = piece_at<kD>(thread / kLanes % kKeys, thread % kLanes * kOut + turn);
 #pragma unroll
     for (int x = 0; x < kLd; ++x) {
       const int item = thread + x * kThreads;
@@ -294,13 +277,9 @@ void prompt_kernel(PromptArgs a) {
       if constexpr (kDirect) {
         dst += piece_at<kD>(item / kLanes % kKeys, item % kLanes ^ swizzle<kD>(item / kLanes % kKeys));
         o[0] = *(lds_u32x4*)dst;
-      } else if constexpr (kKind == 2) {
-        o[0] = widen_fp8<kBf16>(u32x2{data[x].x, data[x].y});
-        o[1] = widen_fp8<kBf16>(u32x2{data[x].z, data[x].w});
-      } else if constexpr (kKind == 3) {
-        const float e = e8m0_scale(exponent[x]);
-#pragma unroll
-        for (int y = 0; y < 4; ++y) o[y] = widen_fp4(data[x][y], e);
+      } else {
+        widen<kBf16, kKind>(data[x], kKind == 3 ? e8m0_scale(exponent[kKind == 3 ? x : 0]) : 0.f,
+                            turn, o);
       }
       // (all of this is put right by every step that may need it, `look`)
       const bool past = look && j * kKeys + item / kLanes % kKeys >= count;
@@ -358,7 +337,7 @@ void prompt_kernel(PromptArgs a) {
   // One step of the wave's rows
   auto compute = [&](int j, const lds_u8* buf) {
     // K piece 2 c + half of row lane & 31 is at at_k ^ 32 c; V piece 4 dc + vpiece of row vrow at
-    // at_v ^ 64 dc, of row vrow + 8 at (at_v ^ 64 dc ^ 32) + 8 rows: formed anew in each step (kept
+    // at_v ^ 64 dc, of row vrow + 8 at (at_v ^ 64 dc ^ 16) + 8 rows: formed anew in each step (kept
     // over the loop they would take two dozen registers)
     uint32_t at_k = piece_at<kD>(lane & 31, half);
     uint32_t at_v = piece_at<kD>(4 * half + (lane & 15) / 4,
@@ -438,10 +417,8 @@ void prompt_kernel(PromptArgs a) {
     auto v_operand = [&](int x) {   // of product x: group x / kDC, values 32 (x % kDC) ..
       const lds_u8* src = vbuf + 16 * (x / kDC) * kRow;
       const int dc = x % kDC;
-      const i16x4 x1 =
-          __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(src + (at_v ^ (dc << 6))));
-      const i16x4 x2 = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-          (lds_i16x4*)(src + (at_v ^ (dc << 6 | 32)) + 8 * kRow));
+      const i16x4 x1 = lds_read_tr16(src + (at_v ^ (dc << 6)));
+      const i16x4 x2 = lds_read_tr16(src + (at_v ^ (dc << 6 | 16)) + 8 * kRow);
       const i16x8 v = {x1[0], x1[1], x1[2], x1[3], x2[0], x2[1], x2[2], x2[3]};
       return __builtin_bit_cast(u32x4, v);
     };

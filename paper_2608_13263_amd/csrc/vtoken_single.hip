@@ -98,7 +98,7 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
   constexpr int kWin = kIT < 32 ? kIT : 32;          // V rows staged per k-step
   constexpr int kPerWin = kWin / kTok > 0 ? kWin / kTok : 1;   // V loads per k-step
   constexpr int kRowK = kRow + 16;                   // LDS bytes per K row
-  constexpr int kRowV = kD * 2 + 32;                 // and per V row (16-bit)
+  constexpr int kRowV = kD * 2;                      // and per V row (16-bit, swizzled)
   constexpr int kWinB = kIT * kRowK > kWin * kRowV ? kIT * kRowK : kWin * kRowV;
   constexpr int kRec = kD + 4;                       // merge: m, l, padding, kD values
   constexpr int kMergeB = kWaves * 16 * kRec * 4;
@@ -263,7 +263,7 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
   const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504088896340736f;
   // this wave's window; only this wave touches it, and a wave's LDS operations run in order, so
   // a compiler fence is all that its reads of other lanes' writes need
-  uint8_t* win = lds + wave * kWinB;
+  lds_u8* const win = (lds_u8*)lds + wave * kWinB;
   auto order_lds = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); };
 
   float m = -INFINITY, l = 0.f;
@@ -276,9 +276,9 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
     // ---- K rows into the window; the next round's K loads
     order_lds();
     {
-      uint8_t* dst = win + (lane / kLanes) * kRowK + (lane % kLanes) * 16;
+      lds_u8* dst = win + (lane / kLanes) * kRowK + (lane % kLanes) * 16;
 #pragma unroll
-      for (int k = 0; k < kLd; ++k) *reinterpret_cast<u32x4*>(dst + k * kTok * kRowK) = kr[k];
+      for (int k = 0; k < kLd; ++k) *(lds_u32x4*)(dst + k * kTok * kRowK) = kr[k];
       if constexpr (kKind == 3) {
         if (lane < kIT) {
           put_exp(exp_s[wave][0][lane], ke);
@@ -305,30 +305,30 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
     f32x4 sc[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      const uint8_t* src = win + (t * 16 + row) * kRowK;
+      const lds_u8* src = win + (t * 16 + row) * kRowK;
       f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};   // two chains of products
       if constexpr (kKind == 3) {
 #pragma unroll
         for (int ch = 0; ch < kChunks; ++ch) {
-          const uint32_t w = *reinterpret_cast<const uint32_t*>(src + grp * (kD / 8) + ch * 4);
+          const uint32_t w = *(const lds_u32*)(src + grp * (kD / 8) + ch * 4);
           const float e = e8m0_scale(exp_s[wave][0][t * 16 + row][(grp * (kD / 4) + ch * 8) / 32]);
           acc[ch & 1] = mfma16<kBf16>(widen_fp4(w, e), qop[ch], acc[ch & 1]);
         }
       } else if constexpr (kPair) {
 #pragma unroll
         for (int ch = 0; ch < kChunks; ch += 2) {
-          const u32x4 w = *reinterpret_cast<const u32x4*>(src + ch * 32 + grp * 16);
+          const u32x4 w = *(const lds_u32x4*)(src + ch * 32 + grp * 16);
           acc[0] = mfma16<kBf16>(widen_fp8<kBf16>(u32x2{w.x, w.y}), qop[ch], acc[0]);
           acc[1] = mfma16<kBf16>(widen_fp8<kBf16>(u32x2{w.z, w.w}), qop[ch + 1], acc[1]);
         }
       } else if constexpr (kKind == 2) {
-        acc[0] = mfma16<kBf16>(widen_fp8<kBf16>(*reinterpret_cast<const u32x2*>(src + grp * 8)),
+        acc[0] = mfma16<kBf16>(widen_fp8<kBf16>(*(const lds_u32x2*)(src + grp * 8)),
                                qop[0], acc[0]);
       } else {
 #pragma unroll
         for (int ch = 0; ch < kChunks; ++ch) {
           acc[ch & 1] = mfma16<kBf16>(
-              *reinterpret_cast<const u32x4*>(src + ch * 64 + grp * 16), qop[ch], acc[ch & 1]);
+              *(const lds_u32x4*)(src + ch * 64 + grp * 16), qop[ch], acc[ch & 1]);
         }
       }
       sc[t] = acc[0] + acc[1];
@@ -379,18 +379,19 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
         const int ld = kHalf ? kc * kWin / kTok : kc * kPerWin + k;
         const int tk = kHalf ? lane / kLanes - (kc * kWin) % kTok : lane / kLanes + k * kTok;
         const u32x4 w = vr[ld];
-        uint8_t* dst = win + tk * kRowV + (lane % kLanes) * (kKind <= 1 ? 16 : kKind == 2 ? 32 : 64);
         if (!kHalf || (tk >= 0 && tk < kWin)) {
-          if constexpr (kKind == 3) {
-            const float e = e8m0_scale(exp_s[wave][1][kc * kWin + tk][lane % kLanes]);
-#pragma unroll
-            for (int y = 0; y < 4; ++y)
-              *reinterpret_cast<u32x4*>(dst + 16 * y) = widen_fp4(w[y], e);
-          } else if constexpr (kKind == 2) {
-            *reinterpret_cast<u32x4*>(dst) = widen_fp8<kBf16>(u32x2{w.x, w.y});
-            *reinterpret_cast<u32x4*>(dst + 16) = widen_fp8<kBf16>(u32x2{w.z, w.w});
+          const int ln = lane % kLanes;
+          if constexpr (kKind <= 1) {
+            *(lds_u32x4*)(win + piece_at<kD>(tk, ln)) = w;
           } else {
-            *reinterpret_cast<u32x4*>(dst) = w;
+            constexpr int kOut = kKind == 2 ? 2 : 4;
+            const int turn = write_turn<kKind, kD>(tk, ln);
+            const uint32_t at = piece_at<kD>(tk, ln * kOut + turn);
+            u32x4 out[kOut];
+            widen<kBf16, kKind>(
+                w, kKind == 3 ? e8m0_scale(exp_s[wave][1][kc * kWin + tk][ln]) : 0.f, turn, out);
+#pragma unroll
+            for (int y = 0; y < kOut; ++y) *(lds_u32x4*)(win + (at ^ (y << 4))) = out[y];
           }
         }
       }
@@ -410,12 +411,13 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
       }
       // V operand rows: lane 16*grp + rho supplies the row of token 4*grp + rho/4 of the first
       // tile (then of the second), elements 4*(rho%4)..+3 of the 16-element chunk
-      const uint8_t* r1 = win + (4 * grp + row / 4) * kRowV + (row % 4) * 8;
+      // (piece 2 dc + .. of the row at r1 ^ 32 dc; 16 rows on the swizzle is the same)
+      const uint32_t r1 = piece_at<kD>(4 * grp + row / 4, row >> 1 & 1) + (row & 1) * 8;
 #pragma unroll
       for (int dc = 0; dc < kDC; ++dc) {
-        const i16x4 x1 = lds_read_tr16(r1 + dc * 32);
+        const i16x4 x1 = lds_read_tr16(win + (r1 ^ (dc << 5)));
         i16x4 x2 = {0, 0, 0, 0};
-        if constexpr (kTiles > 1) x2 = lds_read_tr16(r1 + 16 * kRowV + dc * 32);
+        if constexpr (kTiles > 1) x2 = lds_read_tr16(win + (r1 ^ (dc << 5)) + 16 * kRowV);
         const i16x8 xv = {x1[0], x1[1], x1[2], x1[3], x2[0], x2[1], x2[2], x2[3]};
         o[dc] = mfma16<kBf16>(__builtin_bit_cast(u32x4, xv), __builtin_bit_cast(u32x4, w), o[dc]);
       }
