@@ -3,6 +3,9 @@
 //
 //   single_kernel    one workgroup per (request, KV head, split): scores and the weighted sum of V
 //                    of the query heads that share the KV head, on the matrix cores
+//   shared_kernel    the same for up to four KV heads side by side, where a head's row is less than
+//                    a line
+//   codes_kernel     the same for 4-bit rows
 //   single_combine   merges the splits (no launch where one covers every request)
 //
 // The keys that a query sees are its first min(sinks, ..) ones and its last `window`: a list whose
@@ -79,12 +82,68 @@ __device__ __forceinline__ float groups_reduce(float x) {
   return op(__uint_as_float(s[0]), __uint_as_float(s[1]));
 }
 
+// The waves' sums of each of a workgroup's kHeads heads (wave w: head w % kHeads) into the outputs at
+// `to`, or the split's records. mrg: LDS, [wave][query head][head_dim + 4] floats.
+template <bool kBf16, int kD, int kHeads>
+__device__ __forceinline__ void merge_waves(const PromptArgs& a, float* mrg, float m, float l,
+                                            const f32x4 (&o)[kD / 16], int r, int h0, int split,
+                                            int splits, int64_t to) {
+  using Elem = typename Act<kBf16>::elem;
+  typedef Elem Elem4 __attribute__((ext_vector_type(4)));
+  constexpr int kRec = kD + 4;
+  const int lane = threadIdx.x & 63, grp = lane >> 4, row = lane & 15;
+  const int G = a.group;
+  if (row < G) {
+    float* rec = mrg + ((threadIdx.x >> 6) * 16 + row) * kRec;
+    if (grp == 0) {
+      rec[0] = m;
+      rec[1] = l;
+    }
+#pragma unroll
+    for (int dc = 0; dc < kD / 16; ++dc) {
+      *reinterpret_cast<f32x4*>(rec + 4 + dc * 16 + 4 * grp) = o[dc];
+    }
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < kHeads * G * (kD / 4); i += kThreads) {
+    const int g = i / (kD / 4), d = i % (kD / 4) * 4;   // query head of the workgroup's
+    const float* first = mrg + (g / G * 16 + g % G) * kRec;
+    float top = -INFINITY;
+#pragma unroll
+    for (int w = 0; w < kWaves; w += kHeads) top = fmaxf(top, first[w * 16 * kRec]);
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    float total = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; w += kHeads) {
+      const float* wr = first + w * 16 * kRec;
+      // (a wave whose scores are all NaN has no maximum, but a sum)
+      const float f = wr[0] == -INFINITY ? (wr[1] == 0.f ? 0.f : 1.f)
+                                         : __builtin_amdgcn_exp2f(wr[0] - top);
+      if (f == 0.f) continue;
+      x += *reinterpret_cast<const f32x4*>(wr + 4 + d) * f;
+      total += wr[1] * f;
+    }
+    if (splits == 1) {
+      const f32x4 y = x * (total == 0.f ? 0.f : 1.f / total);
+      *reinterpret_cast<Elem4*>(reinterpret_cast<Elem*>(a.out) + to + g * kD + d) =
+          Elem4{static_cast<Elem>(y.x), static_cast<Elem>(y.y), static_cast<Elem>(y.z),
+                static_cast<Elem>(y.w)};
+      continue;
+    }
+    float* rec = a.workspace +
+                 (((int64_t)r * a.num_kv_heads * G + h0 * G + g) * splits + split) * (kD + 2);
+    *reinterpret_cast<f32x4_in*>(rec + 2 + d) = x;
+    if (d == 0) *reinterpret_cast<f32x2_in*>(rec) = f32x2{top, total};
+  }
+}
+
 template <bool kBf16, int kKind, int kD>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(kD > 128 ? 2 : 3)))
 void single_kernel(PromptArgs a, int split_tokens, int splits) {
   using Elem = typename Act<kBf16>::elem;
   constexpr int kRow = head_bytes(kKind, kD);
+  static_assert(kRow >= 128 && kKind <= 2, "whole lines");
   constexpr int kIT = wave_tokens(kKind, kD);
   constexpr int kStep = kWaves * kIT;                // tokens of a round
   constexpr int kTiles = kIT / 16;                   // 16-token score tiles
@@ -96,17 +155,15 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
   constexpr int kLd = kIT / kTok;                    // loads per operand and round
   constexpr int kSR = (kIT + 63) / 64;               // slot registers
   constexpr int kWin = kIT < 32 ? kIT : 32;          // V rows staged per k-step
-  constexpr int kPerWin = kWin / kTok > 0 ? kWin / kTok : 1;   // V loads per k-step
+  constexpr int kPerWin = kWin / kTok;               // V loads per k-step
   constexpr int kRowK = kRow + 16;                   // LDS bytes per K row
   constexpr int kRowV = kD * 2;                      // and per V row (16-bit, swizzled)
   constexpr int kWinB = kIT * kRowK > kWin * kRowV ? kIT * kRowK : kWin * kRowV;
   constexpr int kRec = kD + 4;                       // merge: m, l, padding, kD values
   constexpr int kMergeB = kWaves * 16 * kRec * 4;
   constexpr int kLdsB = kWaves * kWinB > kMergeB ? kWaves * kWinB : kMergeB;
-  constexpr int kExp = kD / 32;                      // exponents of a head (4-bit rows)
   __shared__ __attribute__((aligned(16))) uint8_t lds[kLdsB];
   __shared__ u32x4 q_s[kChunks][64];
-  __shared__ __attribute__((aligned(8))) uint8_t exp_s[kKind == 3 ? kWaves : 1][2][kIT][kExp];
 
   const int tid = threadIdx.x;
   const int lane = tid & 63;
@@ -114,18 +171,8 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
   const int G = a.group;
   const int H = a.num_kv_heads;
   const int gs = decode_grid_splits(splits);
-  int h, rs;
-  if constexpr (kRow < 128) {
-    // the heads of a split share the lines of their rows: they run on one XCD, eight workgroups
-    // apart
-    const int oct = blockIdx.x / (8 * H);
-    const int x = blockIdx.x - oct * 8 * H;
-    rs = oct * 8 + x % 8;
-    h = x / 8;
-  } else {
-    rs = blockIdx.x % gs + blockIdx.x / (gs * H) * gs;
-    h = blockIdx.x / gs % H;
-  }
+  const int rs = blockIdx.x % gs + blockIdx.x / (gs * H) * gs;
+  const int h = blockIdx.x / gs % H;
   const int r = rs / gs;
   const int split = rs - r * gs;
   if (r >= a.num_reqs || split >= splits) return;
@@ -169,7 +216,6 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
   };
   bool bad = false;   // a slot outside the pool: never dereferenced, poisons the request
   int ls[kLd];        // slots of this lane's rows
-  int own = 0;        // slot of token `lane` (exponents)
   auto spread_slots = [&](Slots x) {
 #pragma unroll
     for (int q = 0; q < kSR; ++q) {
@@ -177,7 +223,6 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
       bad |= !ok;
       x.s[q] = ok ? x.s[q] : 0;
     }
-    own = x.s[0];
 #pragma unroll
     for (int k = 0; k < kLd; ++k) {
       ls[k] = __shfl(x.s[k * kTok / 64], (k * kTok + lane / kLanes) & 63, 64);
@@ -188,50 +233,16 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
 #pragma unroll
     for (int k = 0; k < kLd; ++k) {
       const u32x4* src = reinterpret_cast<const u32x4*>(plane + ((int64_t)ls[k] * a.row_bytes + lane0));
-      if constexpr (kRow < 128) {
-        x[k] = *src;   // its line is read by the other heads too
-      } else {
-        x[k] = __builtin_nontemporal_load(src);
-      }
+      x[k] = __builtin_nontemporal_load(src);
     }
   };
-  // the head's exponents of token `lane`
-  const int64_t exp0 = (int64_t)H * kRow + h * kExp;
-  auto load_exp = [&](const uint8_t* plane) {
-    const uint8_t* src = plane + ((int64_t)own * a.row_bytes + exp0);
-    if constexpr (kExp == 8) {
-      // two words: a head's eight exponents are aligned to eight bytes
-      return *reinterpret_cast<const u32x2*>(src);
-    } else if constexpr (kExp == 4) {
-      return u32x2{*reinterpret_cast<const uint32_t*>(src), 0u};
-    } else if constexpr (kExp == 2) {
-      return u32x2{*reinterpret_cast<const uint16_t*>(src), 0u};
-    } else {
-      return u32x2{*src, 0u};
-    }
-  };
-  auto put_exp = [&](uint8_t* dst, u32x2 x) {
-    if constexpr (kExp == 8) {
-      *reinterpret_cast<u32x2*>(dst) = x;
-    } else if constexpr (kExp == 4) {
-      *reinterpret_cast<uint32_t*>(dst) = x.x;
-    } else if constexpr (kExp == 2) {
-      *reinterpret_cast<uint16_t*>(dst) = static_cast<uint16_t>(x.x);
-    } else {
-      *dst = static_cast<uint8_t>(x.x);
-    }
-  };
-
   Slots cur = load_slots(0);
   Slots nxt = load_slots(1);
   // The head dims of a k-chunk's lane group: any assignment gives the same dot products as long as
-  // q and K use the same one. A lane's pieces of fp8 (of a pair of chunks) and 4-bit rows (of all
-  // of them) are contiguous.
-  constexpr bool kPair = kKind == 2 && kChunks % 2 == 0;
+  // q and K use the same one. A lane's two pieces of fp8 of a pair of chunks are contiguous.
+  constexpr bool kPair = kKind == 2;
   auto head_dim_of = [&](int ch) {
-    return kKind == 3 ? grp * (kD / 4) + ch * 8
-           : kPair    ? (ch >> 1) * 64 + grp * 16 + (ch & 1) * 8
-                      : ch * 32 + grp * 8;
+    return kPair ? (ch >> 1) * 64 + grp * 16 + (ch & 1) * 8 : ch * 32 + grp * 8;
   };
   const Elem* qrow = reinterpret_cast<const Elem*>(a.q) + v.row * a.q_stride +
                      (int64_t)(h * G + (row < G ? row : 0)) * kD;
@@ -242,12 +253,9 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
     qraw[x] = *reinterpret_cast<const u32x4*>(qrow + head_dim_of(ch));
   }
   u32x4 kr[kLd], vr[kLd];
-  u32x2 ke = {}, ve = {};
   spread_slots(cur);
   load_rows(kplane, kr);
-  if constexpr (kKind == 3) ke = load_exp(kplane);
   load_rows(vplane, vr);
-  if constexpr (kKind == 3) ve = load_exp(vplane);
   __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
   for (int x = 0; x < (kChunks + kWaves - 1) / kWaves; ++x) {
@@ -279,21 +287,11 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
       lds_u8* dst = win + (lane / kLanes) * kRowK + (lane % kLanes) * 16;
 #pragma unroll
       for (int k = 0; k < kLd; ++k) *(lds_u32x4*)(dst + k * kTok * kRowK) = kr[k];
-      if constexpr (kKind == 3) {
-        if (lane < kIT) {
-          put_exp(exp_s[wave][0][lane], ke);
-          put_exp(exp_s[wave][1][lane], ve);
-        }
-      }
     }
     order_lds();
     if constexpr (kMore) {
       spread_slots(nxt);
       load_rows(kplane, kr);
-      if constexpr (kKind == 3) {
-        ke = load_exp(kplane);
-        ve = load_exp(vplane);
-      }
       nxt = load_slots(i + 2);
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -307,23 +305,13 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
     for (int t = 0; t < kTiles; ++t) {
       const lds_u8* src = win + (t * 16 + row) * kRowK;
       f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};   // two chains of products
-      if constexpr (kKind == 3) {
-#pragma unroll
-        for (int ch = 0; ch < kChunks; ++ch) {
-          const uint32_t w = *(const lds_u32*)(src + grp * (kD / 8) + ch * 4);
-          const float e = e8m0_scale(exp_s[wave][0][t * 16 + row][(grp * (kD / 4) + ch * 8) / 32]);
-          acc[ch & 1] = mfma16<kBf16>(widen_fp4(w, e), qop[ch], acc[ch & 1]);
-        }
-      } else if constexpr (kPair) {
+      if constexpr (kPair) {
 #pragma unroll
         for (int ch = 0; ch < kChunks; ch += 2) {
           const u32x4 w = *(const lds_u32x4*)(src + ch * 32 + grp * 16);
           acc[0] = mfma16<kBf16>(widen_fp8<kBf16>(u32x2{w.x, w.y}), qop[ch], acc[0]);
           acc[1] = mfma16<kBf16>(widen_fp8<kBf16>(u32x2{w.z, w.w}), qop[ch + 1], acc[1]);
         }
-      } else if constexpr (kKind == 2) {
-        acc[0] = mfma16<kBf16>(widen_fp8<kBf16>(*(const lds_u32x2*)(src + grp * 8)),
-                               qop[0], acc[0]);
       } else {
 #pragma unroll
         for (int ch = 0; ch < kChunks; ++ch) {
@@ -374,25 +362,17 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
       order_lds();
 #pragma unroll
       for (int k = 0; k < kPerWin; ++k) {
-        // (a load of 64 tokens holds two steps' rows: half of the lanes write each)
-        constexpr bool kHalf = kTok > kWin;
-        const int ld = kHalf ? kc * kWin / kTok : kc * kPerWin + k;
-        const int tk = kHalf ? lane / kLanes - (kc * kWin) % kTok : lane / kLanes + k * kTok;
-        const u32x4 w = vr[ld];
-        if (!kHalf || (tk >= 0 && tk < kWin)) {
-          const int ln = lane % kLanes;
-          if constexpr (kKind <= 1) {
-            *(lds_u32x4*)(win + piece_at<kD>(tk, ln)) = w;
-          } else {
-            constexpr int kOut = kKind == 2 ? 2 : 4;
-            const int turn = write_turn<kKind, kD>(tk, ln);
-            const uint32_t at = piece_at<kD>(tk, ln * kOut + turn);
-            u32x4 out[kOut];
-            widen<kBf16, kKind>(
-                w, kKind == 3 ? e8m0_scale(exp_s[wave][1][kc * kWin + tk][ln]) : 0.f, turn, out);
-#pragma unroll
-            for (int y = 0; y < kOut; ++y) *(lds_u32x4*)(win + (at ^ (y << 4))) = out[y];
-          }
+        const u32x4 w = vr[kc * kPerWin + k];
+        const int tk = lane / kLanes + k * kTok, ln = lane % kLanes;
+        if constexpr (kKind <= 1) {
+          *(lds_u32x4*)(win + piece_at<kD>(tk, ln)) = w;
+        } else {
+          const int turn = write_turn<kKind, kD>(tk, ln);
+          const uint32_t at = piece_at<kD>(tk, ln * 2 + turn);
+          u32x4 out[2];
+          widen<kBf16, kKind>(w, 0.f, turn, out);
+          *(lds_u32x4*)(win + at) = out[0];
+          *(lds_u32x4*)(win + (at ^ 16)) = out[1];
         }
       }
       order_lds();
@@ -430,48 +410,630 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
   l = groups_reduce<false>(l);
   if (__ballot(bad) != 0 && rounds > 0) l = __builtin_nanf("");
   __syncthreads();  // the windows are reused for the merge
-  float* mrg = reinterpret_cast<float*>(lds);        // [wave][head][kRec]
-  if (row < G) {
-    float* rec = mrg + (wave * 16 + row) * kRec;
-    if (grp == 0) {
-      rec[0] = m;
-      rec[1] = l;
+  merge_waves<kBf16, kD, 1>(a, reinterpret_cast<float*>(lds), m, l, o, r, h, split, splits, to);
+}
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+
+// 16 tokens x 128 head dims x 16 columns of 4-bit K as it is stored, a lane's 32 codes (one exponent's)
+// of token lane % 16, by 8-bit queries with an exponent of their own per lane.
+__device__ __forceinline__ f32x4 mfma_codes(u32x4 k, uint32_t k_exp, i32x8 q, uint32_t q_exp,
+                                            f32x4 acc) {
+  const i32x8 x = {static_cast<int>(k.x), static_cast<int>(k.y), static_cast<int>(k.z),
+                   static_cast<int>(k.w), 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, q, acc, 4, 0, 0,
+                                                          static_cast<int>(k_exp), 0,
+                                                          static_cast<int>(q_exp));
+}
+
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+
+// bf16 query values as two e4m3 parts each, x = (hi + lo) 2^(e - 127): the upper four and the lower four
+// of a value's eight bits; exact for values down to 2^-9 of the largest, to 2^-17 of it below.
+template <int kN>
+__device__ __forceinline__ void query_parts(const u32x4 (&w)[kN][4], float most, i32x8 (&hi)[kN],
+                                            i32x8 (&lo)[kN], uint32_t& e) {
+  e = max((__float_as_int(most) >> 23) - 7, 1);   // the largest becomes 128 to 256
+  const float inverse = __int_as_float((254 - e) << 23);
+#pragma unroll
+  for (int x = 0; x < kN; ++x)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float y[4];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t u = w[x][i / 2][i % 2 * 2 + j];
+        y[2 * j] = __uint_as_float(u << 16) * inverse;
+        y[2 * j + 1] = __uint_as_float(u & 0xffff0000u) * inverse;
+      }
+      int h = 0, r = 0;
+      h = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], h, false);
+      h = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], h, true);
+      const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(h, false);
+      const f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8(h, true);
+      r = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] - a.x, y[1] - a.y, r, false);
+      r = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] - b.x, y[3] - b.y, r, true);
+      hi[x][i] = h;
+      lo[x][i] = r;
+    }
+}
+
+template <bool kBf16>
+__device__ __forceinline__ f32x4 mfma16x16(i16x4 x, i16x4 y, f32x4 acc) {
+  if constexpr (kBf16) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(x, y, acc, 0, 0, 0);
+  } else {
+    typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
+    return __builtin_amdgcn_mfma_f32_16x16x16f16(__builtin_bit_cast(f16x4, x),
+                                                 __builtin_bit_cast(f16x4, y), acc, 0, 0, 0);
+  }
+}
+
+// LDS of shared_kernel: the round's K and V rows as stored, a window of widened V rows per wave.
+constexpr int shared_window(int kind, int head_dim) {   // rows
+  const int pieces = head_bytes(kind, head_dim) / 16;
+  return pieces < 4 ? 64 / pieces : 16;
+}
+constexpr int shared_lds_bytes(int kind, int head_dim, int heads) {
+  const int step = wave_tokens(kind, head_dim) * kWaves / heads;
+  return 2 * step * (head_bytes(kind, head_dim) * heads + 16) +
+         kWaves * shared_window(kind, head_dim) * head_dim * 2;
+}
+
+// Head rows of less than a line. Wave w takes head w % kHeads of the workgroup's kHeads, and of a
+// round's tokens the (w / kHeads)-th kIT; the workgroup loads the round's rows together, whole lines
+// of all its heads at a time, and passes them through LDS as they are stored.
+template <bool kBf16, int kKind, int kD, int kHeads>
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(
+    kD > 128 || shared_lds_bytes(kKind, kD, kHeads) > 160 * 1024 / 3 ? 2 : 3)))
+void shared_kernel(PromptArgs a, int split_tokens, int splits) {
+  using Elem = typename Act<kBf16>::elem;
+  typedef Elem Elem4 __attribute__((ext_vector_type(4)));
+  constexpr int kRow = head_bytes(kKind, kD);        // bytes of a head's row
+  constexpr int kIT = wave_tokens(kKind, kD);        // tokens of a wave in a round
+  constexpr int kTG = kWaves / kHeads;               // waves of a head
+  constexpr int kStep = kIT * kTG;                   // tokens of a round
+  constexpr int kTW = kStep / kWaves;                // of which a wave loads
+  constexpr int kLanes = kRow * kHeads / 16;         // loads: lanes per token
+  constexpr int kTok = 64 / kLanes;                  // and tokens per instruction
+  constexpr int kLd = kTW / kTok;
+  constexpr int kSR = (kTW + 63) / 64;
+  constexpr int kRaw = kRow * kHeads + 16;           // LDS bytes of a token as stored
+  constexpr int kTiles = kIT / 16;
+  constexpr int kChunks = kD / 32;                   // score k-steps (1 or 2; not of codes)
+  constexpr int kDC = kD / 16;
+  constexpr int kPieces = kRow / 16;                 // 16-byte pieces of a head's row
+  constexpr int kWin = shared_window(kKind, kD);             // V rows widened at a time
+  constexpr int kPer = kWin * kPieces / 64;          // pieces of a lane per window
+  constexpr int kRec = kD + 4;
+  constexpr int kRawB = kStep * kRaw;
+  constexpr int kWinB = kWin * kD * 2;
+  constexpr int kUse = shared_lds_bytes(kKind, kD, kHeads);
+  static_assert(kUse == 2 * kRawB + kWaves * kWinB && kKind <= 2, "LDS");
+  constexpr int kMergeB = kWaves * 16 * kRec * 4;
+  static_assert(kLd * kTok == kTW && kPer * 64 == kWin * kPieces && kIT % kWin == 0, "geometry");
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kUse > kMergeB ? kUse : kMergeB];
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hw = wave % kHeads, tg = wave / kHeads;
+  const int G = a.group;
+  const int H = a.num_kv_heads;
+  const int HG = H / kHeads;
+  const int gs = decode_grid_splits(splits);
+  // head groups that share lines run on one XCD, eight workgroups apart
+  const int oct = blockIdx.x / (8 * HG);
+  const int in_oct = blockIdx.x - oct * 8 * HG;
+  const int rs = oct * 8 + in_oct % 8;
+  const int h0 = in_oct / 8 * kHeads;
+  const int r = rs / gs;
+  const int split = rs - r * gs;
+  if (r >= a.num_reqs || split >= splits) return;
+  const View v = view_of(a, r);
+  const int t0 = split * split_tokens;
+  if (v.ql == 0) return;
+  const int64_t to = v.row * a.out_stride + (int64_t)h0 * G * kD;   // the workgroup's heads
+  if (v.fixed) {
+    if (split != 0) return;
+    const Elem fill = static_cast<Elem>(v.n == 0 && v.s0 >= 0 && v.ql == 1 ? 0.f
+                                                                            : __builtin_nanf(""));
+    for (int i = 0; i < v.ql; ++i) {
+      for (int d = tid; d < kHeads * G * kD; d += kThreads) {
+        reinterpret_cast<Elem*>(a.out)[to + i * a.out_stride + d] = fill;
+      }
+    }
+    return;
+  }
+  if (t0 >= v.count) return;
+  const int nt = min(split_tokens, v.count - t0);
+  const int rounds = (nt + kStep - 1) / kStep;
+  const uint8_t* kplane = a.kv + (int64_t)(2 * a.layer) * a.plane_bytes;
+  const uint8_t* vplane = kplane + a.plane_bytes;
+  const int grp = lane >> 4;    // operand k-group / result row group
+  const int row = lane & 15;    // token of a tile (K operand) / column (Q, P, results)
+
+  // slots of the tokens that this wave loads; those past the split's end re-read its last one
+  struct Slots {
+    int s[kSR];
+  };
+  const int32_t* slots = a.slots + v.s0;
+  auto load_slots = [&](int i) {
+    Slots x;
+#pragma unroll
+    for (int q = 0; q < kSR; ++q) {
+      const int in_wave = kTW < 64 ? lane % kTW : q * 64 + lane;
+      const int t = t0 + min(i * kStep + wave * kTW + in_wave, nt - 1);
+      x.s[q] = slots[t + (t < v.sk ? 0 : v.skip)];
+    }
+    return x;
+  };
+  bool bad = false;   // a slot outside the pool: never dereferenced, poisons the request
+  u32x4 kr[kLd], vr[kLd];
+  const uint32_t row_bytes = static_cast<uint32_t>(a.row_bytes);
+  auto load_rows = [&](Slots x) {
+#pragma unroll
+    for (int q = 0; q < kSR; ++q) {
+      const bool ok = static_cast<unsigned>(x.s[q]) < static_cast<unsigned>(a.num_slots);
+      bad |= !ok;
+      x.s[q] = ok ? x.s[q] : 0;
     }
 #pragma unroll
-    for (int dc = 0; dc < kDC; ++dc) {
-      *reinterpret_cast<f32x4*>(rec + 4 + dc * 16 + 4 * grp) = o[dc];
+    for (int k = 0; k < kLd; ++k) {
+      const uint32_t slot = __shfl(x.s[k * kTok / 64], (k * kTok + lane / kLanes) & 63, 64);
+      const uint64_t at = (uint64_t)slot * row_bytes + h0 * kRow + (lane % kLanes) * 16;
+      kr[k] = *reinterpret_cast<const u32x4*>(kplane + at);
+      vr[k] = *reinterpret_cast<const u32x4*>(vplane + at);
+    }
+  };
+
+  Slots nxt = load_slots(0);
+  // ---- the query operand of the wave's head (any assignment of head dims to chunks gives the same
+  // products as long as K has it too: a lane's piece of K is contiguous in its row)
+  u32x4 q[kChunks];
+  {
+    const Elem* src = reinterpret_cast<const Elem*>(a.q) + v.row * a.q_stride +
+                      (int64_t)((h0 + hw) * G + (row < G ? row : 0)) * kD;
+#pragma unroll
+    for (int ch = 0; ch < kChunks; ++ch) {
+      q[ch] = *reinterpret_cast<const u32x4*>(
+          src + (kKind == 2 ? grp * (kChunks > 1 ? 16 : 8) + ch * 8 : grp * 8));
+      if (a.scale < 0.f) q[ch] ^= 0x80008000u;
+      if (row >= G || a.scale == 0.f) q[ch] = u32x4{0, 0, 0, 0};
     }
   }
-  __syncthreads();
-  for (int i = tid; i < G * (kD / 4); i += kThreads) {
-    const int g = i / (kD / 4), d = i % (kD / 4) * 4;
-    float top = -INFINITY;
+  load_rows(nxt);
+  nxt = load_slots(1);
+  // weights are powers of two, with a positive factor
+  const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504088896340736f;
+  lds_u8* const kraw = (lds_u8*)lds;
+  lds_u8* const vraw = kraw + kRawB;
+  lds_u8* const win = vraw + kRawB + wave * kWinB;
+  auto order_lds = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); };
+
+  float m = -INFINITY, l = 0.f;
+  f32x4 o[kDC];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, mrg[(w * 16 + g) * kRec]);
-    f32x4 x = {0.f, 0.f, 0.f, 0.f};
-    float total = 0.f;
+  for (int dc = 0; dc < kDC; ++dc) o[dc] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  for (int i = 0; i < rounds; ++i) {
+    // ---- the round's rows to LDS, where the last round's have been read (its second barrier)
+    {
+      const uint32_t at = (wave * kTW + lane / kLanes) * kRaw + lane % kLanes * 16;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float* wr = mrg + (w * 16 + g) * kRec;
-      // (a wave whose scores are all NaN has no maximum, but a sum)
-      const float f = wr[0] == -INFINITY ? (wr[1] == 0.f ? 0.f : 1.f)
-                                         : __builtin_amdgcn_exp2f(wr[0] - top);
-      if (f == 0.f) continue;
-      x += *reinterpret_cast<const f32x4*>(wr + 4 + d) * f;
-      total += wr[1] * f;
+      for (int k = 0; k < kLd; ++k) {
+        *(lds_u32x4*)(kraw + at + k * kTok * kRaw) = kr[k];
+        *(lds_u32x4*)(vraw + at + k * kTok * kRaw) = vr[k];
+      }
     }
-    if (splits == 1) {
-      typedef Elem Elem4 __attribute__((ext_vector_type(4)));
-      const f32x4 y = x * (total == 0.f ? 0.f : 1.f / total);
-      *reinterpret_cast<Elem4*>(reinterpret_cast<Elem*>(a.out) + to + g * kD + d) =
-          Elem4{static_cast<Elem>(y.x), static_cast<Elem>(y.y), static_cast<Elem>(y.z),
-                static_cast<Elem>(y.w)};
-      continue;
+    __syncthreads();
+    if (i + 1 < rounds) {
+      load_rows(nxt);
+      nxt = load_slots(i + 2);
     }
-    float* rec = a.workspace + (((int64_t)r * H * G + h * G + g) * splits + split) * (kD + 2);
-    *reinterpret_cast<f32x4_in*>(rec + 2 + d) = x;
-    if (d == 0) *reinterpret_cast<f32x2_in*>(rec) = f32x2{top, total};
+    // ---- scores: lane holds tokens 16 t + 4*grp + j of its column's head
+    const int base_tok = tg * kIT;
+    f32x4 sc[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      const int tk = base_tok + t * 16 + row;
+      const lds_u8* src = kraw + tk * kRaw + hw * kRow;
+      f32x4 acc[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};   // two chains of products
+      if constexpr (kKind == 2) {
+        if constexpr (kChunks > 1) {
+          const u32x4 w = *(const lds_u32x4*)(src + grp * 16);
+          acc[0] = mfma16<kBf16>(widen_fp8<kBf16>(u32x2{w.x, w.y}), q[0], acc[0]);
+          acc[1] = mfma16<kBf16>(widen_fp8<kBf16>(u32x2{w.z, w.w}), q[kChunks - 1], acc[1]);
+          sc[t] = acc[0] + acc[1];
+        } else {
+          sc[t] = mfma16<kBf16>(widen_fp8<kBf16>(*(const lds_u32x2*)(src + grp * 8)), q[0], acc[0]);
+        }
+      } else {
+        sc[t] = mfma16<kBf16>(*(const lds_u32x4*)(src + grp * 16), q[0], acc[0]);
+      }
+    }
+    const int left = nt - (i * kStep + base_tok);   // tokens of the wave's round that exist
+    if (left < kIT) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (16 * t + 4 * grp + j >= left) sc[t][j] = -INFINITY;
+        }
+    }
+    // ---- softmax weights, as in single_kernel
+    float top = sc[0][0];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) top = fmaxf(top, sc[t][j]);
+    top = groups_reduce<true>(top) * scale;
+    if (__ballot(top > m + 8.f) != 0) {
+      const float next = top > m ? top : m;
+      const float f = next == m ? 1.f : __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      l *= f;
+#pragma unroll
+      for (int dc = 0; dc < kDC; ++dc) o[dc] *= f;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+    i16x4 w[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      Elem4 x;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][j], scale, -base));
+        l += p;
+        x[j] = static_cast<Elem>(p);
+      }
+      w[t] = __builtin_bit_cast(i16x4, x);
+    }
+    // ---- O += V^T . P^T, a window of V rows at a time
+#pragma unroll
+    for (int y = 0; y < kIT / kWin; ++y) {
+      u32x4 vw[kPer];
+#pragma unroll
+      for (int x = 0; x < kPer; ++x) {
+        const int tk = base_tok + y * kWin + (x * 64 + lane) / kPieces, ln = lane % kPieces;
+        vw[x] = *(const lds_u32x4*)(vraw + tk * kRaw + hw * kRow + ln * 16);
+      }
+      if (y == kIT / kWin - 1) __syncthreads();   // the round's rows have been read
+      order_lds();
+#pragma unroll
+      for (int x = 0; x < kPer; ++x) {
+        const int tk = (x * 64 + lane) / kPieces, ln = lane % kPieces;
+        if constexpr (kKind <= 1) {
+          *(lds_u32x4*)(win + piece_at<kD>(tk, ln)) = vw[x];
+        } else {
+          const int turn = write_turn<kKind, kD>(tk, ln);
+          const uint32_t at = piece_at<kD>(tk, ln * 2 + turn);
+          u32x4 out[2];
+          widen<kBf16, kKind>(vw[x], 0.f, turn, out);
+          *(lds_u32x4*)(win + at) = out[0];
+          *(lds_u32x4*)(win + (at ^ 16)) = out[1];
+        }
+      }
+      order_lds();
+      // V operand rows: lane 16*grp + rho supplies the row of token 4*grp + rho/4, elements
+      // 4*(rho%4)..+3 of the 16-element chunk
+      const uint32_t r1 = piece_at<kD>(4 * grp + row / 4, row >> 1 & 1) + (row & 1) * 8;
+#pragma unroll
+      for (int t = 0; t < kWin / 16; ++t)
+#pragma unroll
+        for (int dc = 0; dc < kDC; ++dc) {
+          const i16x4 x = lds_read_tr16(win + (r1 ^ (dc << 5)) + t * 16 * kD * 2);
+          o[dc] = mfma16x16<kBf16>(x, w[y * (kWin / 16) + t], o[dc]);
+        }
+    }
   }
+
+  // ---- merge the waves of each head: [m, l] and O[query head][d] per wave into LDS
+  l = groups_reduce<false>(l);
+  if (__syncthreads_or(bad) != 0) l = __builtin_nanf("");   // (the buffers are reused for the merge)
+  merge_waves<kBf16, kD, kHeads>(a, reinterpret_cast<float*>(lds), m, l, o, r, h0, split, splits, to);
+}
+
+// 4-bit rows. Wave w takes head w % kHeads of the workgroup's kHeads (whose rows share lines) and, in
+// round i, kIT tokens; no wave waits for another before the merge.
+//
+//   scores   K stays as it is stored: a lane's 16 bytes of codes, 32 head dims of one token with one
+//            exponent, are its operand of a 16 tokens x 128 dims product of 4-bit by 8-bit numbers
+//            with exponents (MFMA 16x16x128). The query's bf16 values go in as two e4m3 parts (see
+//            query_parts). Heads of fewer dims leave blocks of the 128 over: their loads hold the
+//            pieces of 4 / pieces tiles, and a query in the blocks of one tile, zeros in the others,
+//            picks that tile.
+//   values   codes go to LDS (a quarter of the bytes of widened values) and come back transposed
+//            (ds_read_b64_tr_b4: a lane gets one head dim of 16 tokens). They multiply as bf16
+//            without their exponents, which differ from token to token and so go to the weights:
+//            w 2^(e - 127), exact, one set of weights per 32 head dims.
+// (Widened to bf16 on their way into LDS, V took 48 LDS instructions per 64 tokens of 128 dims instead
+// of 16, and K 64 conversions instead of none.)
+template <int kD, int kHeads>
+__global__ __launch_bounds__(kThreads)
+__attribute__((amdgpu_waves_per_eu(kD > 128 ? 2 : 3)))
+void codes_kernel(PromptArgs a, int split_tokens, int splits) {
+  constexpr int kRow = kD / 2;                       // bytes of a head's codes
+  constexpr int kPieces = kD / 32;                   // 16-byte pieces, an exponent each
+  constexpr int kIT = wave_tokens(3, kD);            // tokens of a wave in a round: 64, or 32
+  constexpr int kStep = kIT * kWaves / kHeads;       // tokens of a round
+  constexpr int kTiles = kIT / 16;
+  constexpr int kLd = kIT * kPieces / 64;            // loads of K, and of V
+  constexpr int kVar = kPieces < 4 ? 4 / kPieces : 1;     // tiles of a load: queries in as many places
+  constexpr int kBlk = kPieces > 4 ? kPieces / 4 : 1;     // 128-dim products of a tile
+  constexpr int kKC = kIT / 32;                      // 32-token value k-steps
+  constexpr int kDC = kD / 16;
+  constexpr int kRec = kD + 4;
+  constexpr int kVB = kIT * kRow, kScB = kPieces * kIT * 4;
+  constexpr int kUse = kWaves * (kVB + kScB), kMergeB = kWaves * 16 * kRec * 4;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[kUse > kMergeB ? kUse : kMergeB];
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int hw = wave % kHeads, tg = wave / kHeads;
+  const int G = a.group;
+  const int H = a.num_kv_heads;
+  const int HG = H / kHeads;
+  const int gs = decode_grid_splits(splits);
+  // workgroups whose heads share lines run on one XCD, eight apart
+  const int oct = blockIdx.x / (8 * HG);
+  const int in_oct = blockIdx.x - oct * 8 * HG;
+  const int rs = oct * 8 + in_oct % 8;
+  const int h0 = in_oct / 8 * kHeads;
+  const int r = rs / gs;
+  const int split = rs - r * gs;
+  if (r >= a.num_reqs || split >= splits) return;
+  const View v = view_of(a, r);
+  const int t0 = split * split_tokens;
+  if (v.ql == 0) return;
+  const int64_t to = v.row * a.out_stride + (int64_t)h0 * G * kD;   // the workgroup's heads
+  if (v.fixed) {
+    if (split != 0) return;
+    const __bf16 fill = static_cast<__bf16>(v.n == 0 && v.s0 >= 0 && v.ql == 1
+                                                ? 0.f
+                                                : __builtin_nanf(""));
+    for (int i = 0; i < v.ql; ++i) {
+      for (int d = tid; d < kHeads * G * kD; d += kThreads) {
+        reinterpret_cast<__bf16*>(a.out)[to + i * a.out_stride + d] = fill;
+      }
+    }
+    return;
+  }
+  if (t0 >= v.count) return;
+  const int nt = min(split_tokens, v.count - t0);
+  const int wt0 = tg * kIT;     // this wave's first token of round 0
+  const int rounds = wt0 < nt ? (nt - wt0 + kStep - 1) / kStep : 0;
+  const uint8_t* kplane = a.kv + (int64_t)(2 * a.layer) * a.plane_bytes;
+  const int64_t to_v = a.plane_bytes;
+  const int grp = lane >> 4;    // operand k-group / result row group
+  const int row = lane & 15;    // token of a tile (K operand) / column (Q, P, results)
+
+  // slot of token `lane` of a round; those past the split's end re-read its last one
+  const int32_t* slots = a.slots + v.s0;
+  auto load_slot = [&](int i) {
+    const int t = t0 + min(wt0 + i * kStep + lane % kIT, nt - 1);
+    return slots[t + (t < v.sk ? 0 : v.skip)];
+  };
+  bool bad = false;   // a slot outside the pool: never dereferenced, poisons the request
+  const uint32_t row_bytes = static_cast<uint32_t>(a.row_bytes);
+  const int code0 = (h0 + hw) * kRow, exp0 = H * kRow + (h0 + hw) * kPieces;
+  // load x holds piece `grp` (modulo the head's) of tile x kVar + grp / pieces, or with more than four
+  // pieces piece grp + 4 (x % kBlk) of tile x / kBlk
+  const int sub_tile = kPieces < 4 ? grp / kPieces : 0;
+  const int piece = kPieces < 4 ? grp % kPieces : grp;
+  uint64_t at[kLd / kBlk];     // of the lane's rows
+  uint64_t own = 0;            // of token `lane`'s
+  auto spread_slots = [&](int s) {
+    const bool ok = static_cast<unsigned>(s) < static_cast<unsigned>(a.num_slots);
+    bad |= !ok;
+    s = ok ? s : 0;
+    own = (uint64_t)static_cast<uint32_t>(s) * row_bytes;
+#pragma unroll
+    for (int x = 0; x < kLd / kBlk; ++x) {
+      at[x] = (uint64_t)static_cast<uint32_t>(
+                  __shfl(s, 16 * (x * kVar + sub_tile) + row, 64)) * row_bytes;
+    }
+  };
+  u32x4 kr[kLd], vr[kLd];
+  uint32_t ke[kLd];
+  u32x2 ve;
+  auto load_k = [&] {
+#pragma unroll
+    for (int x = 0; x < kLd; ++x) {
+      const int pc = piece + x % kBlk * 4;
+      const uint8_t* src = kplane + at[x / kBlk];
+      kr[x] = *reinterpret_cast<const u32x4*>(src + code0 + pc * 16);
+      ke[x] = src[exp0 + pc];
+    }
+  };
+  auto load_v = [&] {
+#pragma unroll
+    for (int x = 0; x < kLd; ++x) {
+      vr[x] = *reinterpret_cast<const u32x4*>(kplane + to_v + at[x / kBlk] + code0 +
+                                              (piece + x % kBlk * 4) * 16);
+    }
+    const uint8_t* e = kplane + to_v + own + exp0;
+    if constexpr (kPieces == 8) {
+      ve = *reinterpret_cast<const u32x2*>(e);
+    } else {
+      ve.x = kPieces == 4   ? *reinterpret_cast<const uint32_t*>(e)
+             : kPieces == 2 ? *reinterpret_cast<const uint16_t*>(e)
+                            : *e;
+    }
+  };
+
+  int nxt = load_slot(0);
+  // ---- the query: 8-bit operand, dims 16 grp .. + 15 and 64 + 16 grp .. of a 128-dim product's
+  i32x8 q_hi[kBlk * kVar], q_lo[kBlk * kVar];
+  uint32_t q_exp;
+  {
+    const uint16_t* src = reinterpret_cast<const uint16_t*>(a.q) + v.row * a.q_stride +
+                          (int64_t)((h0 + hw) * G + (row < G ? row : 0)) * kD;
+    const bool zero = row >= G || a.scale == 0.f;
+    const uint32_t sign = a.scale < 0.f ? 0x80008000u : 0u;
+    u32x4 w[kBlk * kVar][4];
+    int top = 0;
+#pragma unroll
+    for (int x = 0; x < kBlk * kVar; ++x)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        // block of 32 dims of the product; with variants, x places the head's blocks from x pieces on
+        const int block = 2 * (y / 2) + (grp >> 1);
+        const int mine = kVar > 1 ? block - x * kPieces : x * 4 + block;
+        const bool none = zero || mine < 0 || mine >= kPieces;
+        w[x][y] = *reinterpret_cast<const u32x4*>(src + (none ? 0 : mine * 32) + (grp & 1) * 16 +
+                                                  (y & 1) * 8);
+        w[x][y] ^= sign;
+        if (none) w[x][y] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          top = max(top, static_cast<int>(w[x][y][z] & 0x7fff0000u));
+          top = max(top, static_cast<int>(w[x][y][z] << 16 & 0x7fff0000u));
+        }
+      }
+    const float most = groups_reduce<true>(__int_as_float(top));   // over the query's dims
+    query_parts(w, most, q_hi, q_lo, q_exp);
+  }
+  spread_slots(nxt);
+  load_k();
+  load_v();
+  nxt = load_slot(1);
+  // weights are powers of two, with a positive factor
+  const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504088896340736f;
+  // this wave's LDS; its operations run in order, so a compiler fence is all that its reads of other
+  // lanes' writes need
+  lds_u8* const vraw = (lds_u8*)lds + wave * kVB;
+  lds_u8* const scales = (lds_u8*)lds + kWaves * kVB + wave * kScB;   // [piece][token] floats
+  auto order_lds = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); };
+  // piece p of token tk, so that the transpose reads of 16 tokens spread over the banks
+  auto code_at = [](int tk, int p) {
+    const int f = kPieces == 8   ? tk >> 1 & 7
+                  : kPieces == 4 ? tk >> 2 & 3
+                  : kPieces == 2 ? tk >> 3 & 1
+                                 : 0;
+    return tk * kRow + (p ^ f) * 16;
+  };
+
+  float m = -INFINITY, l = 0.f;
+  f32x4 o[kDC];
+#pragma unroll
+  for (int dc = 0; dc < kDC; ++dc) o[dc] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  for (int i = 0; i < rounds; ++i) {
+    // ---- V's codes and exponents to LDS
+    order_lds();
+#pragma unroll
+    for (int x = 0; x < kLd; ++x) {
+      *(lds_u32x4*)(vraw + code_at(16 * (x / kBlk * kVar + sub_tile) + row,
+                                   piece + x % kBlk * 4)) = vr[x];
+    }
+    if (lane < kIT) {
+      typedef __attribute__((address_space(3))) float lds_float;
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p) {
+        *(lds_float*)(scales + (p * kIT + lane) * 4) = e8m0_scale(ve[p / 4] >> (8 * (p % 4)) & 255);
+      }
+    }
+    order_lds();
+    // ---- scores: lane holds tokens 16 t + 4*grp + j of its column's head
+    f32x4 sc[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) sc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < kLd; ++x)
+#pragma unroll
+      for (int y = 0; y < kVar; ++y) {
+        const int t = kVar > 1 ? x * kVar + y : x / kBlk;
+        const int at_q = kVar > 1 ? y : x % kBlk;
+        sc[t] = mfma_codes(kr[x], ke[x], q_hi[at_q], q_exp, sc[t]);
+        sc[t] = mfma_codes(kr[x], ke[x], q_lo[at_q], q_exp, sc[t]);
+      }
+    if (i + 1 < rounds) {
+      spread_slots(nxt);
+      load_k();
+      load_v();
+      nxt = load_slot(i + 2);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    const int left = nt - (wt0 + i * kStep);   // tokens of the wave's round that exist
+    if (left < kIT) {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (16 * t + 4 * grp + j >= left) sc[t][j] = -INFINITY;
+        }
+    }
+    // ---- softmax weights, as in single_kernel
+    float top = sc[0][0];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) top = fmaxf(top, sc[t][j]);
+    top = groups_reduce<true>(top) * scale;
+    if (__ballot(top > m + 8.f) != 0) {
+      const float next = top > m ? top : m;
+      const float f = next == m ? 1.f : __builtin_amdgcn_exp2f(m - next);
+      m = next;
+      l *= f;
+#pragma unroll
+      for (int dc = 0; dc < kDC; ++dc) o[dc] *= f;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        sc[t][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][j], scale, -base));
+        l += sc[t][j];
+      }
+    // ---- O += V^T . P^T, 32 head dims at a time. Rows of a transpose read: the lane group's tokens
+    // 16 t + 4 grp + j, t = 0 .. 3 of one 16-dim block, or t = 0, 1 of both blocks
+    const int rho_tok = 16 * (row / 4 % kTiles) + 4 * grp + row % 4;
+#pragma unroll
+    for (int p = 0; p < kPieces; ++p) {
+      bf16x8 w[kKC];
+#pragma unroll
+      for (int kc = 0; kc < kKC; ++kc)
+#pragma unroll
+        for (int z = 0; z < 2; ++z) {
+          typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+          const f32x4 e = *(lds_f32x4*)(scales + (p * kIT + 16 * (2 * kc + z) + 4 * grp) * 4);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) w[kc][4 * z + j] = static_cast<__bf16>(sc[2 * kc + z][j] * e[j]);
+        }
+      auto codes = [&](int half) {   // of the piece
+        return __builtin_amdgcn_ds_read_tr4_b64_v2i32(
+            (lds_i32x2*)(vraw + code_at(rho_tok, p) + half * 8));
+      };
+      if constexpr (kKC == 2) {
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const i32x2 x = codes(y);
+#pragma unroll
+          for (int kc = 0; kc < 2; ++kc) {
+            o[2 * p + y] = mfma16<true>(widen_fp4(static_cast<uint32_t>(x[kc]), 1.f),
+                                        __builtin_bit_cast(u32x4, w[kc]), o[2 * p + y]);
+          }
+        }
+      } else {
+        const i32x2 x = codes(row / 8);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          o[2 * p + y] = mfma16<true>(widen_fp4(static_cast<uint32_t>(x[y]), 1.f),
+                                      __builtin_bit_cast(u32x4, w[0]), o[2 * p + y]);
+        }
+      }
+    }
+  }
+
+  // ---- merge the waves of each head: [m, l] and O[query head][d] per wave into LDS
+  l = groups_reduce<false>(l);
+  if (__syncthreads_or(bad) != 0) l = __builtin_nanf("");   // (the buffers are reused for the merge)
+  merge_waves<true, kD, kHeads>(a, reinterpret_cast<float*>(lds), m, l, o, r, h0, split, splits, to);
 }
 
 // Merges the split records of one (request, query head). Bound: latency; the records are shared
@@ -546,18 +1108,25 @@ struct Splits {
   int count;    // of a request that sees as much as any may
 };
 
+// Whether a call takes shared_kernel, and for how many heads at a time.
+bool takes_shared(int kind, int head_dim) { return kind == 3 || head_bytes(kind, head_dim) < 128; }
+int shared_heads(int num_kv_heads) {
+  return num_kv_heads % 4 == 0 ? 4 : num_kv_heads % 2 == 0 ? 2 : 1;
+}
+
 // Units of 32 KiB of K (at least a round) per split, by the estimate of decode_split_units(): the
 // workgroups' rounds through the chip plus half a workgroup's time.
 Splits single_splits(const PromptArgs& a, int kind) {
+  const int heads = takes_shared(kind, a.head_dim) ? shared_heads(a.num_kv_heads) : 1;
   const int head = head_bytes(kind, a.head_dim);
-  const int round = kWaves * wave_tokens(kind, a.head_dim);
-  const int64_t unit_tokens = (32768 / head + round - 1) / round * round;
+  const int round = kWaves * wave_tokens(kind, a.head_dim) / heads;
+  const int64_t unit_tokens = (32768 / (head * heads) + round - 1) / round * round;
   int64_t most = a.max_tokens;
   if (a.window > 0 && (int64_t)a.window + a.sinks < most) most = (int64_t)a.window + a.sinks;
-  const int64_t pairs = (int64_t)a.num_reqs * a.num_kv_heads;
+  const int64_t pairs = (int64_t)a.num_reqs * (a.num_kv_heads / heads);
   const int resident = 256 * (a.head_dim > 128 ? 2 : 3);
   const double start = 3.0;
-  const double unit = 2.0 * unit_tokens * head * resident / 7e6;   // us
+  const double unit = 2.0 * unit_tokens * head * heads * resident / 7e6;   // us
   Splits best{static_cast<int>(unit_tokens), 1};
   double best_time = 0;
   for (int u = 1; u <= 8; u *= 2) {
@@ -572,13 +1141,34 @@ Splits single_splits(const PromptArgs& a, int kind) {
   return best;
 }
 
+using Kernel = void (*)(PromptArgs, int, int);
+
+template <bool kBf16, int kKind, int kD>
+Kernel pick(int num_kv_heads) {
+  if constexpr (kKind == 3) {
+    switch (shared_heads(num_kv_heads)) {
+      case 4: return codes_kernel<kD, 4>;
+      case 2: return codes_kernel<kD, 2>;
+      default: return codes_kernel<kD, 1>;
+    }
+  } else if constexpr (head_bytes(kKind, kD) < 128) {
+    switch (shared_heads(num_kv_heads)) {
+      case 4: return shared_kernel<kBf16, kKind, kD, 4>;
+      case 2: return shared_kernel<kBf16, kKind, kD, 2>;
+      default: return shared_kernel<kBf16, kKind, kD, 1>;
+    }
+  } else {
+    return single_kernel<kBf16, kKind, kD>;
+  }
+}
+
 template <bool kBf16, int kKind>
-auto pick_single(int head_dim) -> void (*)(PromptArgs, int, int) {
+Kernel pick_single(int head_dim, int num_kv_heads) {
   switch (head_dim) {
-    case 32: return single_kernel<kBf16, kKind, 32>;
-    case 64: return single_kernel<kBf16, kKind, 64>;
-    case 128: return single_kernel<kBf16, kKind, 128>;
-    case 256: return single_kernel<kBf16, kKind, 256>;
+    case 32: return pick<kBf16, kKind, 32>(num_kv_heads);
+    case 64: return pick<kBf16, kKind, 64>(num_kv_heads);
+    case 128: return pick<kBf16, kKind, 128>(num_kv_heads);
+    case 256: return pick<kBf16, kKind, 256>(num_kv_heads);
     default: return nullptr;
   }
 }
@@ -595,16 +1185,18 @@ int64_t single_workspace_bytes(const PromptArgs& a, int kind) {
 
 hipError_t launch_single(const PromptArgs& a, bool bf16, int kind, hipStream_t stream) {
   const Splits s = single_splits(a, kind);
-  const int64_t groups =
-      decode_grid_groups((int64_t)a.num_reqs * decode_grid_splits(s.count)) * a.num_kv_heads;
+  const int heads = takes_shared(kind, a.head_dim) ? shared_heads(a.num_kv_heads) : 1;
+  const int64_t groups = decode_grid_groups((int64_t)a.num_reqs * decode_grid_splits(s.count)) *
+                         (a.num_kv_heads / heads);
   const int64_t rows = (int64_t)a.num_reqs * a.num_kv_heads * a.group;
   if (groups > INT32_MAX || rows > INT32_MAX) return hipErrorInvalidValue;
-  void (*kernel)(PromptArgs, int, int) = nullptr;
+  Kernel kernel = nullptr;
+  const int D = a.head_dim, H = a.num_kv_heads;
   switch (kind) {
-    case 0: kernel = pick_single<false, 0>(a.head_dim); break;
-    case 1: kernel = pick_single<true, 1>(a.head_dim); break;
-    case 2: kernel = bf16 ? pick_single<true, 2>(a.head_dim) : pick_single<false, 2>(a.head_dim); break;
-    case 3: kernel = pick_single<true, 3>(a.head_dim); break;
+    case 0: kernel = pick_single<false, 0>(D, H); break;
+    case 1: kernel = pick_single<true, 1>(D, H); break;
+    case 2: kernel = bf16 ? pick_single<true, 2>(D, H) : pick_single<false, 2>(D, H); break;
+    case 3: kernel = pick_single<true, 3>(D, H); break;
     default: break;
   }
   if (kernel == nullptr) return hipErrorInvalidValue;
