@@ -80,6 +80,7 @@ typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
 typedef __attribute__((address_space(3))) u32x2 lds_u32x2;
 typedef __attribute__((address_space(3))) uint32_t lds_u32;
+typedef __attribute__((address_space(3))) uint16_t lds_u16;
 
 // Rows of 16-bit values lie in LDS without padding (loads that write it directly leave none), 16-byte
 // piece c of row r at c ^ swizzle(r): the 16-byte reads of 16 rows at one c, and transpose reads of

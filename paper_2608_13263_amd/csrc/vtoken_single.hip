@@ -413,6 +413,50 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
   merge_waves<kBf16, kD, 1>(a, reinterpret_cast<float*>(lds), m, l, o, r, h, split, splits, to);
 }
 
+// kBytes bytes of a cache row (a power of two; aligned to that, or to 16).
+template <int kBytes>
+struct Exponents {
+  u32x4 w[(kBytes + 15) / 16];
+  __device__ __forceinline__ void load(const uint8_t* p) {
+    if constexpr (kBytes >= 16) {
+#pragma unroll
+      for (int i = 0; i < kBytes / 16; ++i) w[i] = *reinterpret_cast<const u32x4*>(p + 16 * i);
+    } else if constexpr (kBytes == 8) {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+      w[0].x = x.x;
+      w[0].y = x.y;
+    } else {
+      w[0].x = kBytes == 4   ? *reinterpret_cast<const uint32_t*>(p)
+               : kBytes == 2 ? *reinterpret_cast<const uint16_t*>(p)
+                             : *p;
+    }
+  }
+  __device__ __forceinline__ void fetch(const lds_u8* p) {
+    static_assert(kBytes <= 8, "a head's");
+    if constexpr (kBytes == 8) {
+      const u32x2 x = *(const lds_u32x2*)p;
+      w[0].x = x.x;
+      w[0].y = x.y;
+    } else {
+      w[0].x = kBytes == 4 ? *(const lds_u32*)p : kBytes == 2 ? *(const lds_u16*)p : *p;
+    }
+  }
+  __device__ __forceinline__ void store(lds_u8* p) const {
+    if constexpr (kBytes >= 16) {
+#pragma unroll
+      for (int i = 0; i < kBytes / 16; ++i) *(lds_u32x4*)(p + 16 * i) = w[i];
+    } else if constexpr (kBytes == 8) {
+      *(lds_u32x2*)p = u32x2{w[0].x, w[0].y};
+    } else if constexpr (kBytes == 4) {
+      *(lds_u32*)p = w[0].x;
+    } else if constexpr (kBytes == 2) {
+      *(lds_u16*)p = static_cast<uint16_t>(w[0].x);
+    } else {
+      *p = static_cast<uint8_t>(w[0].x);
+    }
+  }
+};
+
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
 // 16 tokens x 128 head dims x 16 columns of 4-bit K as it is stored, a lane's 32 codes (one exponent's)
@@ -736,21 +780,23 @@ void shared_kernel(PromptArgs a, int split_tokens, int splits) {
   merge_waves<kBf16, kD, kHeads>(a, reinterpret_cast<float*>(lds), m, l, o, r, h0, split, splits, to);
 }
 
-// 4-bit rows. Wave w takes head w % kHeads of the workgroup's kHeads (whose rows share lines) and, in
-// round i, kIT tokens; no wave waits for another before the merge.
+// 4-bit rows. Wave w takes head w % kHeads of the workgroup's kHeads and, of a round's tokens, the
+// (w / kHeads)-th kIT; the workgroup loads the round's rows together, the pieces of all its heads of a
+// token side by side, and passes them through LDS as they are stored.
 //
-//   scores   K stays as it is stored: a lane's 16 bytes of codes, 32 head dims of one token with one
-//            exponent, are its operand of a 16 tokens x 128 dims product of 4-bit by 8-bit numbers
-//            with exponents (MFMA 16x16x128). The query's bf16 values go in as two e4m3 parts (see
-//            query_parts). Heads of fewer dims leave blocks of the 128 over: their loads hold the
-//            pieces of 4 / pieces tiles, and a query in the blocks of one tile, zeros in the others,
-//            picks that tile.
-//   values   codes go to LDS (a quarter of the bytes of widened values) and come back transposed
-//            (ds_read_b64_tr_b4: a lane gets one head dim of 16 tokens). They multiply as bf16
-//            without their exponents, which differ from token to token and so go to the weights:
-//            w 2^(e - 127), exact, one set of weights per 32 head dims.
-// (Widened to bf16 on their way into LDS, V took 48 LDS instructions per 64 tokens of 128 dims instead
-// of 16, and K 64 conversions instead of none.)
+//   scores   K stays as it is stored: 16 bytes of codes, 32 head dims of one token with one
+//            exponent, are a lane's operand of a 16 tokens x 128 dims product of 4-bit by 8-bit
+//            numbers with exponents (MFMA 16x16x128). The query's bf16 values go in as two e4m3
+//            parts (see query_parts). Heads of fewer dims leave blocks of the 128 over: a lane group
+//            past the head's pieces holds those of the next tiles, and a query in the blocks of one
+//            tile, zeros in the others, picks that tile.
+//   values   come back from LDS transposed as codes (ds_read_b64_tr_b4: a lane gets one head dim of 16
+//            tokens). They multiply as bf16 without their exponents, which differ from token to
+//            token and so go to the weights: w 2^(e - 127), exact, one set of weights per 32 dims.
+//
+// Bound: HBM and latency. Widened to bf16 on their way into LDS, V took 48 LDS instructions per 64
+// tokens of 128 dims instead of 24, and K 64 conversions instead of none; with each wave loading for
+// itself, its 64-byte pieces and 4-byte exponents came in at 3.5 TB/s with nothing else to do.
 template <int kD, int kHeads>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(kD > 128 ? 2 : 3)))
@@ -759,15 +805,23 @@ void codes_kernel(PromptArgs a, int split_tokens, int splits) {
   constexpr int kPieces = kD / 32;                   // 16-byte pieces, an exponent each
   constexpr int kIT = wave_tokens(3, kD);            // tokens of a wave in a round: 64, or 32
   constexpr int kStep = kIT * kWaves / kHeads;       // tokens of a round
+  constexpr int kTW = kStep / kWaves;                // of which a wave loads
+  constexpr int kLanes = kRow * kHeads / 16;         // loads: lanes per token
+  constexpr int kTok = 64 / kLanes;                  // and tokens per instruction
+  constexpr int kLd = kTW / kTok;
   constexpr int kTiles = kIT / 16;
-  constexpr int kLd = kIT * kPieces / 64;            // loads of K, and of V
-  constexpr int kVar = kPieces < 4 ? 4 / kPieces : 1;     // tiles of a load: queries in as many places
+  constexpr int kVar = kPieces < 4 ? 4 / kPieces : 1;     // tiles of a K read: queries in as many places
   constexpr int kBlk = kPieces > 4 ? kPieces / 4 : 1;     // 128-dim products of a tile
   constexpr int kKC = kIT / 32;                      // 32-token value k-steps
   constexpr int kDC = kD / 16;
   constexpr int kRec = kD + 4;
-  constexpr int kVB = kIT * kRow, kScB = kPieces * kIT * 4;
-  constexpr int kUse = kWaves * (kVB + kScB), kMergeB = kWaves * 16 * kRec * 4;
+  constexpr int kRawK = kRow * kHeads + 16;          // LDS bytes of a token's codes: 16-byte reads
+  constexpr int kRawV = kRow * kHeads + 8;           // of 16 tokens; 8-byte ones of 64
+  constexpr int kExp = kPieces * kHeads;             // exponents of a token
+  constexpr int kVAt = kStep * kRawK, kEAt = kVAt + kStep * kRawV, kScAt = kEAt + 2 * kStep * kExp;
+  constexpr int kScB = kPieces * kIT * 4;
+  constexpr int kUse = kScAt + kWaves * kScB, kMergeB = kWaves * 16 * kRec * 4;
+  static_assert(kLd * kTok == kTW && kScAt % 16 == 0, "geometry");
   __shared__ __attribute__((aligned(16))) uint8_t lds[kUse > kMergeB ? kUse : kMergeB];
 
   const int tid = threadIdx.x;
@@ -804,65 +858,38 @@ void codes_kernel(PromptArgs a, int split_tokens, int splits) {
   }
   if (t0 >= v.count) return;
   const int nt = min(split_tokens, v.count - t0);
-  const int wt0 = tg * kIT;     // this wave's first token of round 0
-  const int rounds = wt0 < nt ? (nt - wt0 + kStep - 1) / kStep : 0;
+  const int wt0 = tg * kIT;     // the first token of a round that this wave computes
+  const int rounds = (nt + kStep - 1) / kStep;
   const uint8_t* kplane = a.kv + (int64_t)(2 * a.layer) * a.plane_bytes;
-  const int64_t to_v = a.plane_bytes;
+  const uint8_t* vplane = kplane + a.plane_bytes;
   const int grp = lane >> 4;    // operand k-group / result row group
   const int row = lane & 15;    // token of a tile (K operand) / column (Q, P, results)
 
-  // slot of token `lane` of a round; those past the split's end re-read its last one
+  // slot of the lane's token of those that this wave loads (lanes past them repeat); tokens past the
+  // split's end re-read its last one
   const int32_t* slots = a.slots + v.s0;
   auto load_slot = [&](int i) {
-    const int t = t0 + min(wt0 + i * kStep + lane % kIT, nt - 1);
+    const int t = t0 + min(i * kStep + wave * kTW + lane % kTW, nt - 1);
     return slots[t + (t < v.sk ? 0 : v.skip)];
   };
   bool bad = false;   // a slot outside the pool: never dereferenced, poisons the request
   const uint32_t row_bytes = static_cast<uint32_t>(a.row_bytes);
-  const int code0 = (h0 + hw) * kRow, exp0 = H * kRow + (h0 + hw) * kPieces;
-  // load x holds piece `grp` (modulo the head's) of tile x kVar + grp / pieces, or with more than four
-  // pieces piece grp + 4 (x % kBlk) of tile x / kBlk
-  const int sub_tile = kPieces < 4 ? grp / kPieces : 0;
-  const int piece = kPieces < 4 ? grp % kPieces : grp;
-  uint64_t at[kLd / kBlk];     // of the lane's rows
-  uint64_t own = 0;            // of token `lane`'s
-  auto spread_slots = [&](int s) {
+  u32x4 kr[kLd], vr[kLd];
+  Exponents<kExp> ke, ve;
+  auto load_rows = [&](int s) {
     const bool ok = static_cast<unsigned>(s) < static_cast<unsigned>(a.num_slots);
     bad |= !ok;
     s = ok ? s : 0;
-    own = (uint64_t)static_cast<uint32_t>(s) * row_bytes;
 #pragma unroll
-    for (int x = 0; x < kLd / kBlk; ++x) {
-      at[x] = (uint64_t)static_cast<uint32_t>(
-                  __shfl(s, 16 * (x * kVar + sub_tile) + row, 64)) * row_bytes;
+    for (int k = 0; k < kLd; ++k) {
+      const uint32_t slot = __shfl(s, k * kTok + lane / kLanes, 64);
+      const uint64_t at = (uint64_t)slot * row_bytes + h0 * kRow + lane % kLanes * 16;
+      kr[k] = *reinterpret_cast<const u32x4*>(kplane + at);
+      vr[k] = *reinterpret_cast<const u32x4*>(vplane + at);
     }
-  };
-  u32x4 kr[kLd], vr[kLd];
-  uint32_t ke[kLd];
-  u32x2 ve;
-  auto load_k = [&] {
-#pragma unroll
-    for (int x = 0; x < kLd; ++x) {
-      const int pc = piece + x % kBlk * 4;
-      const uint8_t* src = kplane + at[x / kBlk];
-      kr[x] = *reinterpret_cast<const u32x4*>(src + code0 + pc * 16);
-      ke[x] = src[exp0 + pc];
-    }
-  };
-  auto load_v = [&] {
-#pragma unroll
-    for (int x = 0; x < kLd; ++x) {
-      vr[x] = *reinterpret_cast<const u32x4*>(kplane + to_v + at[x / kBlk] + code0 +
-                                              (piece + x % kBlk * 4) * 16);
-    }
-    const uint8_t* e = kplane + to_v + own + exp0;
-    if constexpr (kPieces == 8) {
-      ve = *reinterpret_cast<const u32x2*>(e);
-    } else {
-      ve.x = kPieces == 4   ? *reinterpret_cast<const uint32_t*>(e)
-             : kPieces == 2 ? *reinterpret_cast<const uint16_t*>(e)
-                            : *e;
-    }
+    const uint64_t at = (uint64_t)static_cast<uint32_t>(s) * row_bytes + H * kRow + h0 * kPieces;
+    ke.load(kplane + at);
+    ve.load(vplane + at);
   };
 
   int nxt = load_slot(0);
@@ -897,25 +924,16 @@ void codes_kernel(PromptArgs a, int split_tokens, int splits) {
     const float most = groups_reduce<true>(__int_as_float(top));   // over the query's dims
     query_parts(w, most, q_hi, q_lo, q_exp);
   }
-  spread_slots(nxt);
-  load_k();
-  load_v();
+  load_rows(nxt);
   nxt = load_slot(1);
   // weights are powers of two, with a positive factor
   const float scale = a.scale == 0.f ? 1.f : fabsf(a.scale) * 1.44269504088896340736f;
-  // this wave's LDS; its operations run in order, so a compiler fence is all that its reads of other
-  // lanes' writes need
-  lds_u8* const vraw = (lds_u8*)lds + wave * kVB;
-  lds_u8* const scales = (lds_u8*)lds + kWaves * kVB + wave * kScB;   // [piece][token] floats
+  lds_u8* const kraw = (lds_u8*)lds;
+  lds_u8* const vraw = kraw + kVAt;
+  lds_u8* const exps = kraw + kEAt;                    // [K, V][token][head][piece]
+  lds_u8* const scales = kraw + kScAt + wave * kScB;   // of the wave's head, [piece][token] floats
+  // a wave's LDS operations run in order: a compiler fence is all that reads of its own writes need
   auto order_lds = [] { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); };
-  // piece p of token tk, so that the transpose reads of 16 tokens spread over the banks
-  auto code_at = [](int tk, int p) {
-    const int f = kPieces == 8   ? tk >> 1 & 7
-                  : kPieces == 4 ? tk >> 2 & 3
-                  : kPieces == 2 ? tk >> 3 & 1
-                                 : 0;
-    return tk * kRow + (p ^ f) * 16;
-  };
 
   float m = -INFINITY, l = 0.f;
   f32x4 o[kDC];
@@ -923,41 +941,56 @@ void codes_kernel(PromptArgs a, int split_tokens, int splits) {
   for (int dc = 0; dc < kDC; ++dc) o[dc] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   for (int i = 0; i < rounds; ++i) {
-    // ---- V's codes and exponents to LDS
-    order_lds();
+    // ---- the round's rows to LDS, where the last round's have been read (its second barrier)
 #pragma unroll
-    for (int x = 0; x < kLd; ++x) {
-      *(lds_u32x4*)(vraw + code_at(16 * (x / kBlk * kVar + sub_tile) + row,
-                                   piece + x % kBlk * 4)) = vr[x];
+    for (int k = 0; k < kLd; ++k) {
+      const int tk = wave * kTW + k * kTok + lane / kLanes;
+      *(lds_u32x4*)(kraw + tk * kRawK + lane % kLanes * 16) = kr[k];
+      lds_u8* dst = vraw + tk * kRawV + lane % kLanes * 16;
+      *(lds_u32x2*)dst = u32x2{vr[k].x, vr[k].y};
+      *(lds_u32x2*)(dst + 8) = u32x2{vr[k].z, vr[k].w};
     }
+    if (lane < kTW) {
+      ke.store(exps + (wave * kTW + lane) * kExp);
+      ve.store(exps + (kStep + wave * kTW + lane) * kExp);
+    }
+    __syncthreads();
+    if (i + 1 < rounds) {
+      load_rows(nxt);
+      nxt = load_slot(i + 2);
+    }
+    // the exponents of V of the wave's tokens as powers of two
     if (lane < kIT) {
       typedef __attribute__((address_space(3))) float lds_float;
+      Exponents<kPieces> e;
+      e.fetch(exps + (kStep + wt0 + lane) * kExp + hw * kPieces);
 #pragma unroll
       for (int p = 0; p < kPieces; ++p) {
-        *(lds_float*)(scales + (p * kIT + lane) * 4) = e8m0_scale(ve[p / 4] >> (8 * (p % 4)) & 255);
+        *(lds_float*)(scales + (p * kIT + lane) * 4) = e8m0_scale(e.w[0][p / 4] >> (8 * (p % 4)) & 255);
       }
     }
     order_lds();
-    // ---- scores: lane holds tokens 16 t + 4*grp + j of its column's head
+    // ---- scores: lane holds tokens 16 t + 4*grp + j of its column's head. Read x holds piece `grp`
+    // (modulo the head's) of tile x kVar + grp / pieces, or, with more than four pieces, piece
+    // grp + 4 (x % kBlk) of tile x / kBlk
     f32x4 sc[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) sc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int x = 0; x < kLd; ++x)
+    for (int x = 0; x < kTiles / kVar * kBlk; ++x) {
+      const int tile = kPieces < 4 ? x * kVar + grp / kPieces : x / kBlk;
+      const int pc = kPieces < 4 ? grp % kPieces : grp + x % kBlk * 4;
+      const int tk = wt0 + 16 * tile + row;
+      const u32x4 k = *(const lds_u32x4*)(kraw + tk * kRawK + hw * kRow + pc * 16);
+      const uint32_t e = exps[tk * kExp + hw * kPieces + pc];
 #pragma unroll
       for (int y = 0; y < kVar; ++y) {
         const int t = kVar > 1 ? x * kVar + y : x / kBlk;
         const int at_q = kVar > 1 ? y : x % kBlk;
-        sc[t] = mfma_codes(kr[x], ke[x], q_hi[at_q], q_exp, sc[t]);
-        sc[t] = mfma_codes(kr[x], ke[x], q_lo[at_q], q_exp, sc[t]);
+        sc[t] = mfma_codes(k, e, q_hi[at_q], q_exp, sc[t]);
+        sc[t] = mfma_codes(k, e, q_lo[at_q], q_exp, sc[t]);
       }
-    if (i + 1 < rounds) {
-      spread_slots(nxt);
-      load_k();
-      load_v();
-      nxt = load_slot(i + 2);
     }
-    __builtin_amdgcn_sched_barrier(0);
     const int left = nt - (wt0 + i * kStep);   // tokens of the wave's round that exist
     if (left < kIT) {
 #pragma unroll
@@ -1007,7 +1040,7 @@ void codes_kernel(PromptArgs a, int split_tokens, int splits) {
         }
       auto codes = [&](int half) {   // of the piece
         return __builtin_amdgcn_ds_read_tr4_b64_v2i32(
-            (lds_i32x2*)(vraw + code_at(rho_tok, p) + half * 8));
+            (lds_i32x2*)(vraw + (wt0 + rho_tok) * kRawV + hw * kRow + p * 16 + half * 8));
       };
       if constexpr (kKC == 2) {
 #pragma unroll
@@ -1028,6 +1061,7 @@ void codes_kernel(PromptArgs a, int split_tokens, int splits) {
         }
       }
     }
+    __syncthreads();   // the round's rows have been read
   }
 
   // ---- merge the waves of each head: [m, l] and O[query head][d] per wave into LDS
