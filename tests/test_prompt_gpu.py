@@ -174,6 +174,26 @@ def test_masked_keys_may_hold_anything(kind):
                     b.abs().max()) + 1e-3
 
 
+@pytest.mark.parametrize("kind,D", [("bf16", 32), ("bf16", 128), ("fp16", 32), ("fp16", 64)])
+def test_infinities_that_are_seen(kind, D):
+    """An infinity of V in a token that a query sees is that output's, of its KV head and value, also
+    where the tokens end inside a tile."""
+    for n in (1, 5, 77, 130, 2049):
+        for queries in ([1], [min(n, 3)]):
+            c = Case(kind, 2, 4, D, [n], queries, seed=6)
+            rows = S.bytes_of(c.cache).clone()
+            last = rows[3][int(c.slots[n - 1])].view(S.TYPES[kind])
+            last[3], last[D + D - 1] = float("inf"), float("-inf")
+            c.cache.kv.view(torch.uint8).reshape(rows.shape).copy_(rows)
+            kw = dict(q_indptr=None, max_queries=1) if queries == [1] else {}
+            got = c.run(0, 0, **kw).cpu()
+            want = torch.zeros(8, D)
+            want[:4, 3], want[4:, D - 1] = float("inf"), float("-inf")
+            sees = got[queries[0] - 1]
+            assert torch.equal(torch.where(torch.isfinite(sees), 0.0, sees.float()), want)
+            assert bool(torch.isfinite(got[: queries[0] - 1]).all())
+
+
 def test_scores_far_apart():
     """Scores over the whole of float32's exponent: one key far above, keys far below; equal scores
     of a large size; a scale of zero and one below zero."""
