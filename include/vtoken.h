@@ -544,8 +544,8 @@ vtoken_status vtoken_read_kv(const vtoken_cache* cache, const vtoken_kv_read* re
  * A query that sees a slot outside the pool gives NaN, no such slot is dereferenced. A request
  * whose slot range is malformed (negative start or count), which holds more than max_tokens slots
  * or more than max_queries queries gives NaN for its queries; one whose query range is
- * not within [0, num_queries] writes nothing. slots may be NULL if no request holds any. A NaN or infinity in K or V reaches the
- * queries that see it and no other.
+ * not within [0, num_queries] writes nothing (the ranges must not overlap). slots may be NULL if no
+ * request holds any. A NaN or infinity in K or V reaches the queries that see it and no other.
  * The work is split over the slots where few queries meet many of them; the partial sums go to the
  * workspace, which is overwritten by every call (calls sharing it must be stream-ordered). */
 typedef struct vtoken_attention {
@@ -556,9 +556,9 @@ typedef struct vtoken_attention {
   const int32_t* slot_count; /* device [num_reqs] or NULL, as in vtoken_decode                     */
   float*       workspace;    /* device, >= vtoken_attention_workspace_bytes() bytes                */
   int64_t      workspace_bytes;
-  int32_t      num_queries;  /* rows of q and out; >= num_reqs without q_indptr                    */
-  int32_t      max_queries;  /* [host] >= every request's queries; 1 without q_indptr              */
-  int32_t      max_tokens;   /* [host] >= the slot count of every request                          */
+  int32_t      num_queries;  /* rows of q and out; >= num_reqs without q_indptr; 2^30 at most      */
+  int32_t      max_queries;  /* [host] >= every request's queries; 1 without q_indptr; <= 2^30     */
+  int32_t      max_tokens;   /* [host] >= the slot count of every request; 2^30 at most            */
   int32_t      num_q_heads;  /* a multiple of num_kv_heads, at most 16 times as many               */
   int32_t      num_kv_heads;
   int32_t      head_dim;     /* 32, 64, 128 or 256                                                 */

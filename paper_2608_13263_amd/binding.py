@@ -900,8 +900,9 @@ def paged_attention(cache: KVCache, q, slot_indptr, slots, layer: int, max_token
     need = lib.vtoken_attention_workspace_bytes(ref, R)   # (-1: the call itself says why)
     if workspace is None and need > 0:
         workspace = torch.empty((need + 3) // 4, dtype=torch.float32, device=dev)
-        if stream is not None and hasattr(stream, "cuda_stream"):
-            workspace.record_stream(stream)
+        if stream is not None:   # (the allocator must not hand it out before that stream is done)
+            workspace.record_stream(stream if hasattr(stream, "cuda_stream") else
+                                    torch.cuda.ExternalStream(int(stream), device=dev))
     if workspace is not None:
         if workspace.device != dev or not workspace.is_contiguous():
             raise ValueError(f"workspace must be contiguous on {dev}")

@@ -742,6 +742,9 @@ vtoken_status vtoken_read_kv(const vtoken_cache* cache, const vtoken_kv_read* r,
 
 namespace {
 
+// Slots of a request and queries of an attention call: sums of a rank and a window fit 32 bits.
+constexpr int32_t kMaxRanks = 1 << 30;
+
 // The sizes of an attention call; fills what the launch and the workspace go by.
 vtoken_status attention_sizes(const vtoken_attention* t, int32_t num_reqs,
                               vtoken::PromptArgs* a) {
@@ -756,6 +759,9 @@ vtoken_status attention_sizes(const vtoken_attention* t, int32_t num_reqs,
   if (D != 32 && D != 64 && D != 128 && D != 256) return VTOKEN_ERR_SHAPE;
   if (t->kv_dtype < 0 || t->kv_dtype > VTOKEN_KV_MXFP4) return VTOKEN_ERR_SHAPE;
   if (t->window < 0 || t->sinks < 0) return VTOKEN_ERR_ARGUMENT;
+  if (t->max_tokens > kMaxRanks || t->num_queries > kMaxRanks || t->max_queries > kMaxRanks) {
+    return VTOKEN_ERR_SHAPE;
+  }
   if (t->q_indptr == nullptr && (t->max_queries != 1 || t->num_queries < num_reqs)) {
     return VTOKEN_ERR_SHAPE;
   }
@@ -769,7 +775,7 @@ vtoken_status attention_sizes(const vtoken_attention* t, int32_t num_reqs,
   a->group = t->num_q_heads / t->num_kv_heads;
   a->head_dim = D;
   a->layer = t->layer;
-  a->window = t->window;
+  a->window = t->window < kMaxRanks ? t->window : kMaxRanks;   // (no rank is further back)
   a->sinks = t->sinks;
   a->scale = t->scale;
   return VTOKEN_OK;

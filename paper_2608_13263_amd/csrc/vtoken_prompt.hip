@@ -47,12 +47,14 @@ __device__ __forceinline__ Request find_request(const PromptArgs& a, int tau) {
   }
   const int lane = threadIdx.x & 63;
   const int tq = tile_tokens(a.group);
+  const int most = (a.max_queries + tq - 1) / tq;
   for (int base = 0; base < a.num_reqs; base += 64) {
     const int r = base + lane;
     const int q0 = r < a.num_reqs ? a.q_indptr[r] : 0;
     const int q1 = r < a.num_reqs ? a.q_indptr[r + 1] : 0;
     const bool ok = q0 >= 0 && q1 > q0 && q1 <= a.num_queries;
-    const int tiles = ok ? (q1 - q0 + tq - 1) / tq : 0;
+    // (one of more queries than the call allows has the tiles of those that it does: the grid's)
+    const int tiles = ok ? min((q1 - q0 + tq - 1) / tq, most) : 0;
     const int incl = meta::wave_inclusive_scan(tiles);
     const uint64_t above = __ballot(incl > tau);
     if (above != 0) {
@@ -159,9 +161,18 @@ void prompt_kernel(PromptArgs a) {
   const int G = a.group;
   const int tq = tile_tokens(G);
   const int i0 = f.tile * tq;
+  if (f.ql > a.max_queries) {   // its queries are NaN, the last tile's and those past it one after the other
+    if (split != 0) return;
+    const int end = f.tile == (a.max_queries + tq - 1) / tq - 1 ? f.ql : i0 + tq;
+    for (int i = i0; i < end; ++i) {
+      Elem* dst = reinterpret_cast<Elem*>(a.out) + (int64_t)(f.q0 + i) * a.out_stride + (int64_t)h * G * kD;
+      for (int d = tid; d < G * kD; d += kThreads) dst[d] = static_cast<Elem>(__builtin_nanf(""));
+    }
+    return;
+  }
   const int s0 = a.slot_indptr[f.r];
   const int n = a.slot_count != nullptr ? a.slot_count[f.r] : a.slot_indptr[f.r + 1] - s0;
-  const bool fixed = s0 < 0 || n < 0 || n > a.max_tokens || f.ql > a.max_queries;
+  const bool fixed = s0 < 0 || n < 0 || n > a.max_tokens;
 
   // ---- this lane's query row, and the keys that the tile's and the wave's rows see
   const int half = lane >> 5;
@@ -553,7 +564,7 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(PromptArgs a, int spl
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int h = blockIdx.x % a.num_kv_heads;
   const Request f = find_request(a, blockIdx.x / a.num_kv_heads);
-  if (f.r < 0) return;
+  if (f.r < 0 || f.ql > a.max_queries) return;   // (the latter's have been written)
   const int G = a.group, D = a.head_dim;
   const int tq = tile_tokens(G);
   const int tokens = min(tq, f.ql - f.tile * tq);
@@ -655,7 +666,7 @@ int64_t prompt_workspace_bytes(const PromptArgs& a, int kind) {
 
 hipError_t launch_prompt(const PromptArgs& a, bool bf16, int kind, hipStream_t stream) {
   const int64_t groups = most_tiles(a) * a.num_kv_heads;
-  if (groups > INT32_MAX) return hipErrorInvalidValue;
+  if (groups > UINT32_MAX / kThreads) return hipErrorInvalidValue;   // (a grid's threads)
   if (groups == 0) return hipSuccess;
   void (*kernel)(PromptArgs) = nullptr;
   switch (kind) {

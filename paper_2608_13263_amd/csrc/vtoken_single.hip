@@ -1238,7 +1238,9 @@ hipError_t launch_single(const PromptArgs& a, bool bf16, int kind, hipStream_t s
   const int64_t groups = decode_grid_groups((int64_t)a.num_reqs * decode_grid_splits(s.count)) *
                          (a.num_kv_heads / heads);
   const int64_t rows = (int64_t)a.num_reqs * a.num_kv_heads * a.group;
-  if (groups > INT32_MAX || rows > INT32_MAX) return hipErrorInvalidValue;
+  if (groups > UINT32_MAX / kThreads || rows > UINT32_MAX / 256) {   // (a grid's threads)
+    return hipErrorInvalidValue;
+  }
   Kernel kernel = nullptr;
   const int D = a.head_dim, H = a.num_kv_heads;
   switch (kind) {

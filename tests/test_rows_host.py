@@ -208,3 +208,12 @@ def test_rotary_table():
         # angles in float64 are off by 2^-52 of 200,000: the cosines by less than a float's step
         assert abs(float(t[p, i]) - math.cos(a)) < 2.0 ** -23
         assert abs(float(t[p, 32 + i]) - math.sin(a)) < 2.0 ** -23
+
+
+@pytest.mark.parametrize("name", ["max_tokens", "max_queries", "num_queries"])
+def test_ranks_past_32_bits_are_refused(name):
+    """Slots of a request and queries up to 2^30: the sum of a rank and a window fits an int32."""
+    lib = B.load_library()
+    for value, ok in ((2 ** 30, True), (2 ** 30 + 1, False), (2 ** 31 - 1, False)):
+        a = _attention(**{name: value})
+        assert (lib.vtoken_attention_workspace_bytes(ctypes.byref(a), 1) >= 0) is ok
