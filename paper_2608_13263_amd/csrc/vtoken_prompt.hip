@@ -358,7 +358,6 @@ void prompt_kernel(PromptArgs a) {
     asm volatile("" : "+v"(at_k), "+v"(at_v));
     // ---- scores: lane holds keys 32 t + 8 (i / 4) + 4 half + i % 4 of its row
     f32x16 s[kTiles];
-    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
@@ -379,7 +378,6 @@ void prompt_kernel(PromptArgs a) {
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
     __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
-    __builtin_amdgcn_s_setprio(0);
     auto key_of = [&](int t, int e) {   // rank of the lane's key, or past every row's
       const int x = j * kKeys + 32 * t + 8 * (e / 4) + 4 * half + e % 4;
       const int k = x + (x < sk ? 0 : skip);
@@ -435,6 +433,7 @@ void prompt_kernel(PromptArgs a) {
       const i16x8 v = {x1[0], x1[1], x1[2], x1[3], x2[0], x2[1], x2[2], x2[3]};
       return __builtin_bit_cast(u32x4, v);
     };
+    __builtin_amdgcn_s_setprio(1);
     constexpr int kProducts = kGroups * kDC;
     u32x4 v[3] = {v_operand(0), v_operand(1 < kProducts ? 1 : 0), {}};
     typename Act<kBf16>::x8 w[2];
@@ -448,6 +447,7 @@ void prompt_kernel(PromptArgs a) {
       if (g + 1 < kGroups) weights(w[(g + 1) & 1], g + 1, dc * kPart, kPart);
       __builtin_amdgcn_sched_barrier(0);
     }
+    __builtin_amdgcn_s_setprio(0);
   };
   // Step j's infinities and NaN of V, which LDS holds as zeros, for the rows that see them (from the
   // cache: this is rare, and a row that sees one is lost anyway)
