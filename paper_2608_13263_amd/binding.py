@@ -11,6 +11,11 @@ GPU, the calls raise.
     build_token_table(cache, batch, plan)
     repack(cache, batch, plan)
     free_blocks(batch, plan)             # plan.freed[:plan.counters[2]]
+
+Around the passes, per layer (KVCache, or PackedKVCache for 4-bit rows):
+
+    q = write_kv(cache, k, v, new_slots, layer, q=q, positions=p, cos_sin=table, k_weight=w, ...)
+    out = paged_attention(cache, q, slot_indptr, slots, layer, max_tokens, q_indptr=..., ...)
 """
 from __future__ import annotations
 
