@@ -545,7 +545,8 @@ vtoken_status vtoken_read_kv(const vtoken_cache* cache, const vtoken_kv_read* re
  * whose slot range is malformed (negative start or count), which holds more than max_tokens slots
  * or more than max_queries queries gives NaN for its queries; one whose query range is
  * not within [0, num_queries] writes nothing (the ranges must not overlap). slots may be NULL if no
- * request holds any. A NaN or infinity in K or V reaches the queries that see it and no other.
+ * request holds any. A NaN or infinity in K or V reaches the queries that see it and no other. Sums
+ * over V are float32 and take weights up to 2^8: values past 2^100 may overflow in them.
  * The work is split over the slots where few queries meet many of them; the partial sums go to the
  * workspace, which is overwritten by every call (calls sharing it must be stream-ordered). */
 typedef struct vtoken_attention {

@@ -138,10 +138,10 @@ __device__ __forceinline__ uint32_t only_finite(uint32_t w) {
 // rounded ones, and the output is rounded once.
 //
 // Measured: 8,192 queries with a window of 4,096, 32 query and 8 KV heads of 128, 16 bits, 412.6 GFLOP:
-// 460 us, 896 TFLOP/s, three quarters of a large library product's 1,202. Counters: matrix cores busy
-// 41% of the time, vector instructions 47%, LDS 22% without conflicts, at 2.08 GHz; HBM idle. Without the
-// exponentials, or with half of the V reads, it takes 3 to 5% less: neither is the bound, the
-// order within a wave and the clock under this load are.
+// 447 us, 924 TFLOP/s, three quarters of a large library product's 1,202. Counters: matrix cores busy
+// 42% of the time, vector instructions 47%, LDS 22% without conflicts, at 2.08 GHz; HBM idle. Without the
+// exponentials, or with half of the V reads, it takes 3 to 5% less, without the loads 15: none of them
+// is the bound, the order within a wave and the clock under this load are.
 // Measured and not kept: 64 rows by 32 keys a wave, which halves the reads of LDS (2,048 queries of 4,096
 // keys 180 us instead of 138, 26 registers spilled; one workgroup per CU, none spilled, 209; 64 dims 90.5
 // instead of 88); scores a step ahead of the weights (16 bits of 128 dims 2 to 7% faster, 8 bits 1% and
@@ -255,33 +255,34 @@ void prompt_kernel(PromptArgs a) {
   u32x4 data[kDirect ? 1 : kLd];
   uint32_t exponent[kKind == 3 ? kLd : 1];
   const uint32_t row_bytes = static_cast<uint32_t>(a.row_bytes);
-  auto load_rows = [&](const uint32_t (&s)[kSl], lds_u8* buf) {
-#pragma unroll
-    for (int x = 0; x < kLd; ++x) {
-      const int item = tid + x * kThreads;
-      if (2 * kItems < kThreads && item >= 2 * kItems) break;
-      const bool is_v = kLd > 1 ? x >= kLd / 2 : item >= kItems;
-      const uint32_t slot = s[x % kSl] < num_slots ? s[x % kSl] : 0u;
-      const int ln = item % kLanes;
-      const uint8_t* plane = is_v ? kplane + a.plane_bytes : kplane;
-      if constexpr (kDirect) {
-        // a wave's 64 pieces follow each other in LDS: the lane picks the piece that belongs there
-        const uint8_t* src = plane +
-                             (h * kLanes + (ln ^ swizzle<kD>(item / kLanes % kKeys))) * 16 +
-                             (uint64_t)slot * row_bytes;
-        typedef __attribute__((address_space(1))) const uint32_t global_u32;
-        typedef __attribute__((address_space(3))) uint32_t lds_u32;
-        __builtin_amdgcn_global_load_lds(
-            (global_u32*)(reinterpret_cast<uintptr_t>(src)),
-            (lds_u32*)(buf + (wave * 64 + x * kThreads) * 16), 16, 0, 0);
-      } else {
-        const uint8_t* row = plane + (uint64_t)slot * row_bytes;
-        data[x] = *reinterpret_cast<const u32x4*>(row + (h * kLanes + ln) * 16);
-        if constexpr (kKind == 3) {
-          exponent[x] = row[a.num_kv_heads * (kD / 2) + h * (kD / 32) + ln];
-        }
+  auto load_row = [&](int x, const uint32_t (&s)[kSl], lds_u8* buf) {   // item x of this thread's
+    const int item = tid + x * kThreads;
+    if (2 * kItems < kThreads && item >= 2 * kItems) return;
+    const bool is_v = kLd > 1 ? x >= kLd / 2 : item >= kItems;
+    const uint32_t slot = s[x % kSl] < num_slots ? s[x % kSl] : 0u;
+    const int ln = item % kLanes;
+    const uint8_t* plane = is_v ? kplane + a.plane_bytes : kplane;
+    if constexpr (kDirect) {
+      // a wave's 64 pieces follow each other in LDS: the lane picks the piece that belongs there
+      const uint8_t* src = plane +
+                           (h * kLanes + (ln ^ swizzle<kD>(item / kLanes % kKeys))) * 16 +
+                           (uint64_t)slot * row_bytes;
+      typedef __attribute__((address_space(1))) const uint32_t global_u32;
+      typedef __attribute__((address_space(3))) uint32_t lds_u32;
+      __builtin_amdgcn_global_load_lds(
+          (global_u32*)(reinterpret_cast<uintptr_t>(src)),
+          (lds_u32*)(buf + (wave * 64 + x * kThreads) * 16), 16, 0, 0);
+    } else {
+      const uint8_t* row = plane + (uint64_t)slot * row_bytes;
+      data[x] = *reinterpret_cast<const u32x4*>(row + (h * kLanes + ln) * 16);
+      if constexpr (kKind == 3) {
+        exponent[x] = row[a.num_kv_heads * (kD / 2) + h * (kD / 32) + ln];
       }
     }
+  };
+  auto load_rows = [&](const uint32_t (&s)[kSl], lds_u8* buf) {
+#pragma unroll
+    for (int x = 0; x < kLd; ++x) load_row(x, s, buf);
   };
   // What step j's rows still need before they can be read: the widened values; where a row is past
   // the list (V: zeros, K: anything) or outside the pool (V: zeros, K: NaN); and where some row does
@@ -368,8 +369,12 @@ void prompt_kernel(PromptArgs a) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) o[dc][e] = 0.f;
 
-  // One step of the wave's rows
-  auto compute = [&](int j, const lds_u8* buf) {
+  uint32_t sa[kSl], sb[kSl];   // slots of this step and, when its rows are asked for, the next
+  // One step of the wave's rows. The next step's rows that go straight to `other` are asked for beside the
+  // first of its value products, one each: all at once, after the barrier, the waves wait for each other's
+  // (4 x 1,024 queries of 8,192 keys of 16 bits 526 us instead of 572; rows that go through registers
+  // 1 to 2% slower that way).
+  auto compute = [&](int j, const lds_u8* buf, lds_u8* other) {
     // K piece 2 c + half of row lane & 31 is at at_k ^ 32 c; V piece 4 dc + vpiece of row vrow at
     // at_v ^ 64 dc, of row vrow + 8 at (at_v ^ 64 dc ^ 16) + 8 rows: formed anew in each step (kept
     // over the loop they would take two dozen registers)
@@ -458,6 +463,7 @@ void prompt_kernel(PromptArgs a) {
     // (a wave in its value products goes first: 4 x 1,024 queries of 8,192 keys in 8 bits 532 us; with that
     // for its scores 559; 16 bits and 128 dims take the same)
     constexpr int kProducts = kGroups * kDC;
+    static_assert(!kDirect || kLd <= kProducts, "a load beside a product");
     u32x4 v[3] = {v_operand(0), v_operand(1 < kProducts ? 1 : 0), {}};
     typename Act<kBf16>::x8 w[2];
     weights(w[0], 0, 0, 8);
@@ -468,6 +474,7 @@ void prompt_kernel(PromptArgs a) {
       if (x + 2 < kProducts) v[(x + 2) % 3] = v_operand(x + 2);
       o[dc] = mfma32<kBf16>(v[x % 3], __builtin_bit_cast(u32x4, w[g & 1]), o[dc]);
       if (g + 1 < kGroups) weights(w[(g + 1) & 1], g + 1, dc * kPart, kPart);
+      if (kDirect && x < kLd) load_row(x, sa, other);
       __builtin_amdgcn_sched_barrier(0);
     }
     __builtin_amdgcn_s_setprio(0);
@@ -501,7 +508,6 @@ void prompt_kernel(PromptArgs a) {
     }
   };
 
-  uint32_t sa[kSl], sb[kSl];
   // Step j from `buf`, the next step's rows on their way to `other`. One barrier a step: `other`
   // was last read in step j - 1, which every wave has left when it passes step j's barrier.
   lds_u8* const buf0 = (lds_u8*)lds0;
@@ -513,13 +519,14 @@ void prompt_kernel(PromptArgs a) {
     const bool more = j + 1 < step1;
     if (!kDirect && more) load_rows(sb, other);
     __syncthreads();
-    if (kDirect && more) load_rows(sb, other);
+    const int k0 = j * kKeys + (j * kKeys < sk ? 0 : skip);
+    const bool none = !w_real || k0 > w_last;
+    if (kDirect && none && more) load_rows(sb, other);
 #pragma unroll
     for (int x = 0; x < kSl; ++x) sa[x] = sb[x];
     if (j + 2 < step1) load_slots(j + 2, sb);
-    const int k0 = j * kKeys + (j * kKeys < sk ? 0 : skip);
-    if (!w_real || k0 > w_last) return;
-    compute(j, buf);
+    if (none) return;
+    compute(j, buf, other);
     if (odd_step[j & 1] == j) add_nonfinite(j);
   };
   if (tid < 2) odd_step[tid] = -1;
@@ -533,6 +540,8 @@ void prompt_kernel(PromptArgs a) {
     step(j, buf0, buf1);
     if (j + 1 < step1) step(j + 1, buf1, buf0);
   }
+  // the last step's loads, which nothing reads, must not outlive the workgroup's LDS
+  if constexpr (kDirect) __builtin_amdgcn_s_waitcnt(0x0f70);
 
   // ---- the rows' results: lane holds values 32 dc + 8 (e / 4) + 4 half + e % 4
   int at_row = m_row;   // (the row's place is worked out again, not kept over the loop)
