@@ -613,10 +613,10 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(PromptArgs a, int spl
   float top = ml.x;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d, 64));
-  // (a split whose scores are all NaN has no maximum, but a sum)
-  const float w = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f)
-                                    : __builtin_amdgcn_exp2f(ml.x - top);
-  float total = w == 0.f ? 0.f : ml.y * w;
+  // (no split is left out: a NaN or an infinity in the sums of one far below the others has to reach
+  // the row, also times zero; one without a maximum holds zeros, or NaN)
+  const float w = ml.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
+  float total = ml.y * w;
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) total += __shfl_xor(total, d, 64);
   const int p0 = 2 * lane, p1 = 128 + 2 * lane;   // this lane's pairs of values
@@ -625,14 +625,14 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(PromptArgs a, int spl
     f32x2 x0[8], x1[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float* src = rec + (s + j < splits ? s + j : s) * rs + 2;
-      x0[j] = p0 < D ? *reinterpret_cast<const f32x2_in*>(src + p0) : f32x2{0.f, 0.f};
-      x1[j] = p1 < D ? *reinterpret_cast<const f32x2_in*>(src + p1) : f32x2{0.f, 0.f};
+      const bool ok = s + j < splits;
+      const float* src = rec + (ok ? s + j : s) * rs + 2;
+      x0[j] = ok && p0 < D ? *reinterpret_cast<const f32x2_in*>(src + p0) : f32x2{0.f, 0.f};
+      x1[j] = ok && p1 < D ? *reinterpret_cast<const f32x2_in*>(src + p1) : f32x2{0.f, 0.f};
     }
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float ws = s + j < splits ? __shfl(w, (s + j) & 63, 64) : 0.f;
-      if (ws == 0.f) continue;
+      const float ws = __shfl(w, (s + j) & 63, 64);
       v0 += x0[j] * ws;
       v1 += x1[j] * ws;
     }

@@ -116,10 +116,9 @@ __device__ __forceinline__ void merge_waves(const PromptArgs& a, float* mrg, flo
 #pragma unroll
     for (int w = 0; w < kWaves; w += kHeads) {
       const float* wr = first + w * 16 * kRec;
-      // (a wave whose scores are all NaN has no maximum, but a sum)
-      const float f = wr[0] == -INFINITY ? (wr[1] == 0.f ? 0.f : 1.f)
-                                         : __builtin_amdgcn_exp2f(wr[0] - top);
-      if (f == 0.f) continue;
+      // (no wave is left out: a NaN or an infinity in the sums of one far below the others has to
+      // reach the row, also times zero; one without a maximum holds zeros, or NaN)
+      const float f = wr[0] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(wr[0] - top);
       x += *reinterpret_cast<const f32x4*>(wr + 4 + d) * f;
       total += wr[1] * f;
     }
@@ -1123,24 +1122,24 @@ __global__ __launch_bounds__(64 * kCW) void single_combine(PromptArgs a, int spl
   float total = 0.f, x[4] = {0.f, 0.f, 0.f, 0.f};
   for (int base = 0; base < ns; base += 64) {
     const f32x2 ml = base == 0 ? first : head_of(base + lane);
-    const float w = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f)
-                                      : __builtin_amdgcn_exp2f(ml.x - top);
-    total += w == 0.f ? 0.f : ml.y * w;
+    // (as in merge_waves: every split counts, also one whose weight is zero)
+    const float w = ml.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
+    total += ml.y * w;
     for (int s = wave; s < 64 && base + s < ns; s += 4 * kCW) {
       float y[4][4], ws[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int t = s + j * kCW;
         const bool ok = t < 64 && base + t < ns;
-        ws[j] = ok ? __shfl(w, t & 63, 64) : 0.f;
+        ws[j] = __shfl(w, t & 63, 64);
         const float* rec = rec0 + (ok ? base + t : base + s) * rs + 2;
 #pragma unroll
-        for (int c = 0; c < 4; ++c) y[j][c] = c * 64 + lane < D ? rec[c * 64 + lane] : 0.f;
+        for (int c = 0; c < 4; ++c) y[j][c] = ok && c * 64 + lane < D ? rec[c * 64 + lane] : 0.f;
       }
 #pragma unroll
       for (int j = 0; j < 4; ++j)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) x[c] += ws[j] == 0.f ? 0.f : ws[j] * y[j][c];
+        for (int c = 0; c < 4; ++c) x[c] += ws[j] * y[j][c];
     }
   }
 #pragma unroll
