@@ -265,6 +265,23 @@ def _stream(stream) -> int:
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory that a call on `stream` writes. Given a stream, it comes from that stream's own: a block
+    of the current stream's may have work of its last owner still to come, which the call would not
+    wait for. It is not handed out again before the current stream has done with it either."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):   # (no stream object is made of the handle 0)
+        raw = _stream(stream)
+        stream = torch.cuda.ExternalStream(raw, device=device) if raw else \
+            torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        x = torch.empty(shape, dtype=dtype, device=device)
+    x.record_stream(torch.cuda.current_stream(device))
+    return x
+
+
 class _Cached:
     """The C struct of an object is built once and reused (it only holds the tensors' device
     addresses and sizes); assigning any attribute drops it. Building the structs costs a few
@@ -808,7 +825,7 @@ def write_kv(cache: KVCache, k, v, slots, layer: int, q=None, positions=None, co
         q_heads = int(q.shape[1]) if q.dim() == 3 else 0
         q_stride = _activation(q, "q", dev, act, q_heads, D, n)
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=act, device=dev)
+            q_out = _empty(q.shape, act, dev, stream)
         out_stride = _activation(q_out, "q_out", dev, act, q_heads, D, n)
     elif q_out is not None:
         raise ValueError("q_out without q")
@@ -848,9 +865,9 @@ def read_kv(cache: KVCache, slots, layer: int, dtype=None, k_out=None, v_out=Non
         dtype = k_out.dtype if k_out is not None else \
             torch.float16 if code == KV_FP16 else torch.bfloat16
     if k_out is None:
-        k_out = torch.empty(n, H, D, dtype=dtype, device=dev)
+        k_out = _empty((n, H, D), dtype, dev, stream)
     if v_out is None:
-        v_out = torch.empty(n, H, D, dtype=dtype, device=dev)
+        v_out = _empty((n, H, D), dtype, dev, stream)
     r = CKVRead(slots.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
                 _activation(k_out, "k_out", dev, dtype, H, D, n),
                 _activation(v_out, "v_out", dev, dtype, H, D, n), n, H, D, layer,
@@ -886,7 +903,7 @@ def paged_attention(cache: KVCache, q, slot_indptr, slots, layer: int, max_token
     R, rows = slot_indptr.numel() - 1, int(q.shape[0])
     stride = _activation(q, "q", dev, act, heads, D)
     if out is None:
-        out = torch.empty(q.shape, dtype=act, device=dev)
+        out = _empty(q.shape, act, dev, stream)
     elif out.shape != q.shape:
         raise ValueError("out must match q")
     if q_indptr is not None:
@@ -904,10 +921,7 @@ def paged_attention(cache: KVCache, q, slot_indptr, slots, layer: int, max_token
     ref = ctypes.byref(a)
     need = lib.vtoken_attention_workspace_bytes(ref, R)   # (-1: the call itself says why)
     if workspace is None and need > 0:
-        workspace = torch.empty((need + 3) // 4, dtype=torch.float32, device=dev)
-        if stream is not None:   # (the allocator must not hand it out before that stream is done)
-            workspace.record_stream(stream if hasattr(stream, "cuda_stream") else
-                                    torch.cuda.ExternalStream(int(stream), device=dev))
+        workspace = _empty((need + 3) // 4, torch.float32, dev, stream)
     if workspace is not None:
         if workspace.device != dev or not workspace.is_contiguous():
             raise ValueError(f"workspace must be contiguous on {dev}")

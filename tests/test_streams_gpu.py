@@ -1,0 +1,104 @@
+"""Calls on a stream that is not the current one, with memory that the binding allocates: work that
+other streams still have to do on blocks they gave back has no part in the results."""
+import pytest
+import torch
+
+from paper_2608_13263_amd import binding as B
+import serving_helpers as S
+from test_prompt_gpu import Case
+
+pytestmark = pytest.mark.gpu
+
+SPIN = 20_000_000   # cycles that a stream is held up for: some milliseconds
+
+
+def _late_writes(sizes):
+    """Blocks of these many bytes go back to the current stream's memory with a write to come."""
+    blocks = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(3)]
+    torch.cuda._sleep(SPIN)
+    for b in blocks:
+        b.fill_(255)   # NaN of every type here
+
+
+def _held_up(stream):
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(SPIN)
+
+
+def _streams():
+    """A stream, and one by its handle."""
+    keep = torch.cuda.Stream(), torch.cuda.Stream()
+    return [(keep[0], keep[0]), (keep[1], keep[1].cuda_stream)]
+
+
+@pytest.mark.parametrize("queries", [[1], [9]])
+def test_attention(queries):
+    c = Case("bf16", 2, 4, 128, [6000], queries, seed=40, extra=0)
+    q, slots = c.q.cuda(), c.slots.cuda()
+    indptr = torch.tensor(c.indptr, dtype=torch.int32).cuda()
+    q_indptr = torch.tensor(c.q_indptr, dtype=torch.int32).cuda()
+
+    def call(stream=None):
+        return B.paged_attention(c.cache, q, indptr, slots, 1, 6000, q_indptr=q_indptr,
+                                 max_queries=queries[0], stream=stream)
+
+    want = call()
+    t = B.CAttention(None, None, 0, 0, q.data_ptr(), None, None, 0, q.shape[0], queries[0], 6000,
+                     8, 2, 128, 1, B.KV_BF16, B.KV_BF16, 0, 0, 1.0)
+    need = B.attention_workspace_bytes(t, 1)
+    assert need > 0
+    torch.cuda.synchronize()
+    for side, given in _streams():
+        for _ in range(2):
+            _late_writes([need, want.numel() * 2])
+            got = call(given)
+            side.synchronize()
+            late = got.clone()
+            torch.cuda.synchronize()
+            assert torch.equal(late, want) and torch.equal(got, want)
+            # blocks asked for right after the call are not its workspace
+            _held_up(side)
+            got = call(given)
+            for n in (need, need, got.numel() * 2):
+                torch.empty(n, dtype=torch.uint8, device="cuda").fill_(255)
+            torch.cuda.synchronize()
+            assert torch.equal(got, want)
+
+
+def test_outputs_that_the_current_stream_still_reads():
+    """An output given back while the current stream has still to read it is not the next call's."""
+    n = 300
+    g = torch.Generator().manual_seed(41)
+    planes = torch.stack([S.make_rows("bf16", 512, 2, 64, g) for _ in range(2)])
+    cache = S.make_cache(B, planes, "bf16", 2, 64, 16)
+    a, b = (torch.randperm(512, generator=g)[:n].to(torch.int32).cuda() for _ in range(2))
+    want = [x.clone() for x in B.read_kv(cache, a, 0)]
+    torch.cuda.synchronize()
+    for side, given in _streams():
+        for _ in range(2):
+            _late_writes([n * 256])
+            k, v = B.read_kv(cache, a, 0, stream=given)
+            torch.cuda.current_stream().wait_stream(side)
+            torch.cuda._sleep(SPIN)
+            got = k.clone(), v.clone()
+            del k, v
+            B.read_kv(cache, b, 0, stream=given)
+            torch.cuda.synchronize()
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_written_queries():
+    n = 200
+    g = torch.Generator().manual_seed(42)
+    planes = torch.stack([S.make_rows("bf16", 512, 2, 64, g) for _ in range(2)])
+    cache = S.make_cache(B, planes, "bf16", 2, 64, 16)
+    x = torch.randn(3, n, 2, 64, generator=g).to(torch.bfloat16).cuda()
+    slots = torch.arange(n, dtype=torch.int32).cuda()
+    kw = dict(q=x[0], positions=slots, cos_sin=B.rotary_table(n, 64))
+    want = B.write_kv(cache, x[1], x[2], slots, 0, **kw)
+    torch.cuda.synchronize()
+    for side, given in _streams():
+        _late_writes([n * 256])
+        got = B.write_kv(cache, x[1], x[2], slots, 0, stream=given, **kw)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
