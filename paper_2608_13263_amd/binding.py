@@ -394,14 +394,15 @@ class Plan(_Cached):
             setattr(self, k, tensors[k])
 
     @classmethod
-    def allocate(cls, batch: Batch, block_size: int, device="cuda", inplace: bool = False):
+    def allocate(cls, batch: Batch, block_size: int, device="cuda", inplace: bool = False,
+                 stream=None):
         """Outputs sized for out-of-place mode, or for in-place mode (src_plan holds up to
-        M destination blocks)."""
+        M destination blocks); `stream`: the one that the passes run on, if not the current one."""
         import torch
         R, T, M, f = batch.num_reqs, batch.num_tokens, batch.num_bt_entries, batch.free_len
 
         def e(n):
-            return torch.empty(max(int(n), 1), dtype=torch.int32, device=device)
+            return _empty(max(int(n), 1), torch.int32, device, stream)
         rows = M if inplace else min(f, M)
         return cls(token_slot=e(T), live_count=e(R), admitted=e(R), dst_indptr=e(R + 1),
                    new_bt_indptr=e(R + 1), new_block_ids=e(M),
@@ -497,8 +498,8 @@ def check_layout(cache: KVCache, batch: Batch, workspace=None, stream=None):
     lib = load_library()
     need = int(lib.vtoken_check_layout_workspace_bytes(cache.num_blocks))
     if workspace is None:
-        workspace = torch.empty(max(need // 4, 1), dtype=torch.int32, device=cache.kv.device)
-    status = torch.empty(1, dtype=torch.int32, device=cache.kv.device)
+        workspace = _empty(max(need // 4, 1), torch.int32, cache.kv.device, stream)
+    status = _empty(1, torch.int32, cache.kv.device, stream)
     c, b = cache.c(), batch.c()
     _check(lib.vtoken_check_layout(ctypes.byref(c), ctypes.byref(b), _ptr(workspace),
                                    int(workspace.numel() * workspace.element_size()),
@@ -512,7 +513,8 @@ def run_pass(cache: KVCache, batch: Batch, plan: Optional[Plan] = None, stream=N
     freed list in one launch (vtoken_repack_free, vtoken_repack_inplace_free). A small pass is
     bound by these calls' host side, so the stream is looked up once."""
     if plan is None:
-        plan = Plan.allocate(batch, cache.block_size, device=cache.kv.device, inplace=inplace)
+        plan = Plan.allocate(batch, cache.block_size, device=cache.kv.device, inplace=inplace,
+                             stream=stream)
     stream = _stream(stream)
     if inplace:
         build_token_table_inplace(cache, batch, plan, stream)
@@ -531,9 +533,9 @@ def build_slot_mapping(batch: Batch, plan: Plan, slot_indptr=None, slots=None,
     lib = load_library()
     dev = plan.counters.device
     if slot_indptr is None:
-        slot_indptr = torch.empty(batch.num_reqs + 1, dtype=torch.int32, device=dev)
+        slot_indptr = _empty(batch.num_reqs + 1, torch.int32, dev, stream)
     if slots is None:
-        slots = torch.empty(max(batch.num_tokens, 1), dtype=torch.int32, device=dev)
+        slots = _empty(max(batch.num_tokens, 1), torch.int32, dev, stream)
     b, p = batch.c(), plan.c()
     _check(lib.vtoken_build_slot_mapping(ctypes.byref(b), ctypes.byref(p), _ptr(slot_indptr),
                                          _ptr(slots), int(slots.numel()), _stream(stream)),
@@ -548,10 +550,9 @@ def build_slot_table(batch: Batch, plan: Plan, reserve: int, stream=None):
     lib = load_library()
     dev = plan.counters.device
     R = batch.num_reqs
-    start = torch.empty(R + 1, dtype=torch.int32, device=dev)
-    count = torch.empty(max(R, 1), dtype=torch.int32, device=dev)
-    slots = torch.empty(max(batch.num_tokens + R * int(reserve), 1), dtype=torch.int32,
-                        device=dev)
+    start = _empty(R + 1, torch.int32, dev, stream)
+    count = _empty(max(R, 1), torch.int32, dev, stream)
+    slots = _empty(max(batch.num_tokens + R * int(reserve), 1), torch.int32, dev, stream)
     b, p = batch.c(), plan.c()
     _check(lib.vtoken_build_slot_table(ctypes.byref(b), ctypes.byref(p), int(reserve),
                                        _ptr(start), _ptr(count), _ptr(slots),
@@ -567,7 +568,7 @@ def append_slots(slot_start, slot_count, slots, append_indptr, append_slots, sta
     import torch
     lib = load_library()
     if status is None:
-        status = torch.empty(1, dtype=torch.int32, device=slots.device)
+        status = _empty(1, torch.int32, slots.device, stream)
     R = int(append_indptr.numel()) - 1
     most = 0 if append_slots is None else int(append_slots.numel())
     _check(lib.vtoken_append_slots_n(R, most, _ptr(append_indptr), _ptr(append_slots),
@@ -610,12 +611,12 @@ def paged_decode(cache: KVCache, q, slot_indptr, slots, layer: int, max_tokens: 
     if D != cache.head_dim:
         raise ValueError("q head_dim differs from the cache's")
     if out is None:
-        out = torch.empty_like(q)
+        out = _empty(q.shape, torch.float32, q.device, stream)
     if out.shape != q.shape or out.dtype != torch.float32 or not out.is_contiguous():
         raise ValueError("out must match q")
     need = decode_workspace_bytes(R, Hq, D, max_tokens)
     if workspace is None:
-        workspace = torch.empty(max(need // 4, 1), dtype=torch.float32, device=q.device)
+        workspace = _empty(max(need // 4, 1), torch.float32, q.device, stream)
     code = kv_dtype_code(cache.kv.dtype) if kv_dtype is None else int(kv_dtype)
     if scale is None:
         scale = D ** -0.5
@@ -686,11 +687,11 @@ class PlannerState:
         self.pinned = pinned
 
     @classmethod
-    def allocate(cls, num_blocks: int, batch: Batch, device="cuda", pinned=None):
+    def allocate(cls, num_blocks: int, batch: Batch, device="cuda", pinned=None, stream=None):
         import torch
 
         def e(n, dt=torch.int32):
-            return torch.empty(max(int(n), 1), dtype=dt, device=device)
+            return _empty(max(int(n), 1), dt, device, stream)
         M, R = batch.num_bt_entries, batch.num_reqs
         if pinned is not None and not isinstance(pinned, torch.Tensor):
             import numpy as np
@@ -721,10 +722,10 @@ def run_partial_pass(cache: KVCache, batch: Batch, slot_in, plan: Optional[Plan]
     """Plan and copy of one partial pass, enqueued in order on one stream; returns
     (plan, state). The released sources are state.sources[:plan.counters[2]]."""
     if plan is None:
-        plan = Plan.allocate(batch, cache.block_size, device=cache.kv.device)
+        plan = Plan.allocate(batch, cache.block_size, device=cache.kv.device, stream=stream)
     if state is None:
         state = PlannerState.allocate(cache.num_blocks, batch, device=cache.kv.device,
-                                      pinned=pinned)
+                                      pinned=pinned, stream=stream)
     stream = _stream(stream)
     plan_partial(cache, batch, slot_in, plan, state, params, stream)
     repack(cache, batch, plan, stream)

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 from paper_2608_13263_amd import binding as B
+from paper_2608_13263_amd import workloads as W
 import serving_helpers as S
 from test_prompt_gpu import Case
 
@@ -102,3 +103,38 @@ def test_written_queries():
         got = B.write_kv(cache, x[1], x[2], slots, 0, stream=given, **kw)
         torch.cuda.synchronize()
         assert torch.equal(got, want)
+
+
+def test_a_pass_and_what_reads_it():
+    """The plan, the layout check, the slot mapping and table, an append's status and the decode."""
+    inp = W.tiny_cache(101)
+    sh = inp.shape
+    batch = B.Batch.from_inputs(inp)
+    kv = W.kv_device(sh, inp.num_blocks, 1)
+    q = torch.randn(inp.num_reqs, 4 * sh.num_kv_heads, sh.head_dim, device="cuda")
+    none = torch.zeros(inp.num_reqs + 1, dtype=torch.int32, device="cuda")
+
+    def run(stream=None):
+        cache = B.KVCache(kv.clone(), sh.num_layers, sh.num_kv_heads, sh.head_dim, sh.block_size)
+        torch.cuda.synchronize()
+        if stream is not None:
+            _late_writes([4, 64, 512, 4096, 1 << 15, 1 << 16, 1 << 20])
+        status = B.check_layout(cache, batch, stream=stream)
+        plan = B.run_pass(cache, batch, stream=stream)
+        indptr, slots = B.build_slot_mapping(batch, plan, stream=stream)
+        table = B.build_slot_table(batch, plan, 4, stream=stream)
+        full = B.append_slots(*table, none, none, stream=stream)
+        out = B.paged_decode(cache, q, indptr, slots, 0, 4096, stream=stream)
+        torch.cuda.synchronize()
+        n, held = int(indptr[-1]), int(plan.new_bt_indptr[-1])
+        assert int(status) == 0 and int(full) == 0 and int(plan.counters[3]) == 0 and n > 0
+        rows = [t for r in range(inp.num_reqs) for t in
+                table[2][int(table[0][r]): int(table[0][r]) + int(table[1][r])].tolist()]
+        return (indptr, slots[:n], table[0], table[1], torch.tensor(rows), out,
+                plan.new_block_ids[:held], plan.freed[: int(plan.counters[2])],
+                plan.token_slot[: inp.num_tokens], cache.kv.view(torch.uint8))
+
+    want = run()
+    for side, given in _streams():
+        for a, b in zip(run(given), want):
+            assert torch.equal(a, b)
