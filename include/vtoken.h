@@ -501,7 +501,7 @@ typedef struct vtoken_kv_write {
   int32_t      num_kv_heads;
   int32_t      head_dim;
   int32_t      rotary_dim;   /* a multiple of 16 (of 8 if interleaved), <= head_dim                */
-  int32_t      num_positions;
+  int32_t      num_positions;  /* rows of cos_sin, at least one                                    */
   int32_t      interleaved;  /* 0 or 1                                                             */
   int32_t      layer;
   int32_t      dtype;        /* VTOKEN_KV_FP16 or VTOKEN_KV_BF16                                   */

@@ -840,6 +840,8 @@ def write_kv(cache: KVCache, k, v, slots, layer: int, q=None, positions=None, co
         if cos_sin.dtype != torch.float32 or cos_sin.device != dev or cos_sin.dim() != 2 or \
                 not cos_sin.is_contiguous():
             raise ValueError(f"cos_sin must be contiguous float32 [positions][rotary_dim] on {dev}")
+        if cos_sin.numel() == 0:   # (its null pointer would mean no table: keys stored unturned)
+            raise ValueError("cos_sin has no angles")
         _ints(positions, "positions", dev, n)
         num_positions, rotary = cos_sin.shape
     w = CKVWrite(_ptr(q), k.data_ptr(), v.data_ptr(), _ptr(q_out), q_stride,

@@ -653,7 +653,7 @@ vtoken_status vtoken_write_kv(const vtoken_cache* cache, const vtoken_kv_write* 
   if (w->num_tokens < 0 || w->num_q_heads < 0) return VTOKEN_ERR_SHAPE;
   if (w->interleaved != 0 && w->interleaved != 1) return VTOKEN_ERR_ARGUMENT;
   if (w->cos_sin != nullptr &&
-      (w->rotary_dim <= 0 || w->rotary_dim > D || w->num_positions < 0 ||
+      (w->rotary_dim <= 0 || w->rotary_dim > D || w->num_positions <= 0 ||
        w->rotary_dim % (w->interleaved != 0 ? 8 : 16) != 0)) {
     return VTOKEN_ERR_SHAPE;
   }

@@ -2,6 +2,7 @@
 work, and the binding's own checks."""
 import ctypes
 import os
+from types import SimpleNamespace
 
 import pytest
 import torch
@@ -217,3 +218,16 @@ def test_ranks_past_32_bits_are_refused(name):
     for value, ok in ((2 ** 30, True), (2 ** 30 + 1, False), (2 ** 31 - 1, False)):
         a = _attention(**{name: value})
         assert (lib.vtoken_attention_workspace_bytes(ctypes.byref(a), 1) >= 0) is ok
+
+
+def test_a_table_without_positions_is_refused():
+    """Every position is outside of it, and there is no row to read in a bad one's place."""
+    for tokens in (0, 2):
+        st = _status("vtoken_write_kv", _write(num_positions=0, num_tokens=tokens), None, None)
+        assert st == CODE["VTOKEN_ERR_SHAPE"]
+    cache = SimpleNamespace(kv=torch.zeros(2, 1, 16, 2, 64, dtype=torch.bfloat16), num_kv_heads=2,
+                            head_dim=64)
+    x, i = torch.zeros(3, 2, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    for shape in ((0, 64), (10, 0)):
+        with pytest.raises(ValueError, match="no angles"):
+            B.write_kv(cache, x, x, i, 0, positions=i, cos_sin=torch.zeros(shape))
