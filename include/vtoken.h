@@ -482,7 +482,7 @@ int64_t vtoken_kv_row_bytes(int32_t num_kv_heads, int32_t head_dim, int32_t kv_d
  * A negative slot marks padding: nothing of that token is written. A slot past the pool,
  * or a position outside [0, num_positions) where there is a table, writes nothing to the cache and
  * NaN to the token's q_out. Slots of a call must differ (of two tokens with one slot, which values
- * stay is not defined). A call may have 2^27 head rows of q, k and v over all tokens (more:
+ * stay is not defined). A call may have 2^27 - 8 head rows of q, k and v over all tokens (more:
  * VTOKEN_ERR_SHAPE). */
 typedef struct vtoken_kv_write {
   const void*  q;            /* device [num_tokens][num_q_heads][head_dim]; NULL if num_q_heads 0  */
@@ -515,7 +515,7 @@ vtoken_status vtoken_write_kv(const vtoken_cache* cache, const vtoken_kv_write* 
 /* The K and V rows of listed slots of one layer as dense tensors (a request's cache exported, or
  * looked at): k_out[i], v_out[i] = values at slots[i], exact in dtype (4-bit values outside bf16's
  * range aside). A slot outside the pool reads as NaN. Slots may repeat. A call may have
- * 2^27 head rows of K and V (more: VTOKEN_ERR_SHAPE). */
+ * 2^27 - 8 head rows of K and V (more: VTOKEN_ERR_SHAPE). */
 typedef struct vtoken_kv_read {
   const int32_t* slots;      /* device [num_tokens]                                                */
   void*        k_out;        /* device [num_tokens][num_kv_heads][head_dim]                        */

@@ -629,8 +629,9 @@ vtoken_status check_activation(const void* p, int64_t stride, int64_t width, int
   return VTOKEN_OK;
 }
 
-// Head rows (of q, k and v, over all tokens) that one call may have.
-constexpr int64_t kMaxHeadRows = 1LL << 27;
+// Head rows (of q, k and v, over all tokens) that one call may have: at 32 lanes each, in whole
+// workgroups of eight, the grid's threads stay below 2^32.
+constexpr int64_t kMaxHeadRows = (1LL << 27) - 8;
 
 int64_t plane_bytes_of(const vtoken_cache* c) {
   return (int64_t)c->num_blocks * c->block_size * c->num_kv_heads * c->head_dim * c->elem_bytes;
@@ -657,7 +658,6 @@ vtoken_status vtoken_write_kv(const vtoken_cache* cache, const vtoken_kv_write* 
        w->rotary_dim % (w->interleaved != 0 ? 8 : 16) != 0)) {
     return VTOKEN_ERR_SHAPE;
   }
-  // (32 lanes at most to a head row: thread indexes fit 32 bits)
   const int64_t rows = (int64_t)w->num_q_heads + 2 * (int64_t)w->num_kv_heads;
   if (rows > kMaxHeadRows / (w->num_tokens > 0 ? w->num_tokens : 1)) return VTOKEN_ERR_SHAPE;
   if (w->num_tokens == 0) return VTOKEN_OK;

@@ -231,3 +231,16 @@ def test_a_table_without_positions_is_refused():
     for shape in ((0, 64), (10, 0)):
         with pytest.raises(ValueError, match="no angles"):
             B.write_kv(cache, x, x, i, 0, positions=i, cos_sin=torch.zeros(shape))
+
+
+def test_most_head_rows():
+    """2^27 - 8 head rows, 32 lanes each at 256 dims, are a grid of less than 2^32 threads; a call of
+    one more row is refused before the launch (slots of NULL are looked at later)."""
+    c = _cache(num_kv_heads=1, head_dim=256)
+    w = dict(num_q_heads=0, num_kv_heads=1, head_dim=256, rotary_dim=256, slots=None)
+    r = dict(num_kv_heads=1, head_dim=256, slots=None)
+    for tokens, code in ((2 ** 26 - 4, "NULL"), (2 ** 26 - 3, "SHAPE"), (2 ** 26, "SHAPE")):
+        assert _status("vtoken_write_kv", _write(num_tokens=tokens, **w), c,
+                       None) == CODE["VTOKEN_ERR_" + code]
+        assert _status("vtoken_read_kv", _read(num_tokens=tokens, **r), c,
+                       None) == CODE["VTOKEN_ERR_" + code]
