@@ -789,7 +789,7 @@ int64_t vtoken_attention_workspace_bytes(const vtoken_attention* t, int32_t num_
   vtoken::PromptArgs a;
   if (t == nullptr || attention_sizes(t, num_reqs, &a) != VTOKEN_OK) return -1;
   return a.max_queries == 1 ? vtoken::single_workspace_bytes(a, t->kv_dtype)
-                            : vtoken::prompt_workspace_bytes(a, t->kv_dtype);
+                            : vtoken::prompt_workspace_bytes(a);
 }
 
 vtoken_status vtoken_paged_attention(const vtoken_cache* cache, const vtoken_attention* t,

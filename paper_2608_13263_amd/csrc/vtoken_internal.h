@@ -430,7 +430,7 @@ struct PromptArgs {
   const uint8_t* q;
   uint8_t* out;
   int64_t q_stride, out_stride;   // elements
-  const int32_t* q_indptr;        // null: one query per request
+  const int32_t* q_indptr;        // null: one query per request (vtoken_single.hip only)
   const int32_t* slot_indptr;
   const int32_t* slots;
   const int32_t* slot_count;      // null: counts from slot_indptr
@@ -448,7 +448,7 @@ struct PromptArgs {
   int32_t sinks;
   float scale;
 };
-int64_t prompt_workspace_bytes(const PromptArgs& a, int kind);
+int64_t prompt_workspace_bytes(const PromptArgs& a);
 hipError_t launch_prompt(const PromptArgs& a, bool bf16, int kind, hipStream_t stream);
 // The same where no request has more than one query (vtoken_single.hip).
 int64_t single_workspace_bytes(const PromptArgs& a, int kind);

@@ -45,10 +45,6 @@ struct Request {
 // gets the answer; 64 requests at a time.
 __device__ __forceinline__ Request find_request(const PromptArgs& a, int tau) {
   Request f{-1, 0, 0, 0};
-  if (a.q_indptr == nullptr) {
-    if (tau < a.num_reqs) f = Request{tau, tau, 1, 0};
-    return f;
-  }
   const int lane = threadIdx.x & 63;
   const int tq = tile_tokens(a.group);
   const int most = (a.max_queries + tq - 1) / tq;
@@ -651,7 +647,6 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(PromptArgs a, int spl
 
 // Tiles of query rows that a batch can have.
 int64_t most_tiles(const PromptArgs& a) {
-  if (a.q_indptr == nullptr) return a.num_reqs;
   const int tq = tile_tokens(a.group);
   const int64_t by_rows = a.num_queries / tq + (int64_t)a.num_reqs;
   const int64_t by_reqs = (int64_t)a.num_reqs * ((a.max_queries + tq - 1) / tq);
@@ -691,7 +686,7 @@ auto pick_prompt(int head_dim) -> void (*)(PromptArgs) {
 
 }  // namespace
 
-int64_t prompt_workspace_bytes(const PromptArgs& a, int kind) {
+int64_t prompt_workspace_bytes(const PromptArgs& a) {
   const int splits = prompt_splits(a);
   if (splits == 1) return 0;
   return (int64_t)a.num_queries * a.num_kv_heads * a.group * splits * (a.head_dim + 2) * 4;
@@ -700,7 +695,6 @@ int64_t prompt_workspace_bytes(const PromptArgs& a, int kind) {
 hipError_t launch_prompt(const PromptArgs& a, bool bf16, int kind, hipStream_t stream) {
   const int64_t groups = most_tiles(a) * a.num_kv_heads;
   if (groups > UINT32_MAX / kThreads) return hipErrorInvalidValue;   // (a grid's threads)
-  if (groups == 0) return hipSuccess;
   void (*kernel)(PromptArgs) = nullptr;
   switch (kind) {
     case 0: kernel = pick_prompt<false, 0>(a.head_dim); break;

@@ -349,7 +349,6 @@ hipError_t launch_rows(const Args& a, int64_t tokens, int64_t parts, int head_di
                        int kind, hipStream_t stream) {
   const int lanes = row_lanes(head_dim);
   const int64_t groups = (tokens * parts * lanes + kRowThreads - 1) / kRowThreads;
-  if (groups * kRowThreads > UINT32_MAX) return hipErrorInvalidValue;   // (thread indexes)
   void (*kernel)(Args) = nullptr;
   auto pick = [&](auto lanes_t) {
     constexpr int kLanes = decltype(lanes_t)::value;
