@@ -539,14 +539,15 @@ vtoken_status vtoken_read_kv(const vtoken_cache* cache, const vtoken_kv_read* re
  *   k <= p  and  (window == 0  or  k > p - window  or  k < sinks),
  * ranks counted in the mapping's order, over the live tokens only. Query head qh reads KV head
  * qh / (num_q_heads / num_kv_heads). out = softmax(scale * q . K^T) @ V, sums and softmax in
- * float32, weights in dtype for the product with V, rounded once to dtype; a query that sees
- * nothing (ql > n) gives zeros. Rows of q past the last query are neither read nor written.
+ * float32, weights in dtype for the product with V (fp16: to 2^-36 of the row's largest at the
+ * finest), rounded once to dtype; a query that sees nothing (ql > n), or whose scores are all
+ * -infinity, gives zeros. Rows of q past the last query are neither read nor written.
  * A query that sees a slot outside the pool gives NaN, no such slot is dereferenced. A request
  * whose slot range is malformed (negative start or count), which holds more than max_tokens slots
  * or more than max_queries queries gives NaN for its queries; one whose query range is
  * not within [0, num_queries] writes nothing (the ranges must not overlap). slots may be NULL if no
  * request holds any. A NaN or infinity in K or V reaches the queries that see it and no other. Sums
- * over V are float32 and take weights up to 2^8: values past 2^100 may overflow in them.
+ * over V are float32 and take weights up to 2^8 (fp16: 2^15): values past 2^100 may overflow in them.
  * The work is split over the slots where few queries meet many of them; the partial sums go to the
  * workspace, which is overwritten by every call (calls sharing it must be stream-ordered). */
 typedef struct vtoken_attention {

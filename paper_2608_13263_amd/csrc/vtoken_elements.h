@@ -23,15 +23,21 @@ typedef f32x4 f32x4_in __attribute__((aligned(4)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef short i16x8 __attribute__((ext_vector_type(8)));
 
-// The 16-bit type of activations and of matrix-core operands.
+// The 16-bit type of activations and of matrix-core operands. Softmax weights are 2^(x - m): m follows
+// a row's maximum, to kFirst below it, where that passes m + kMost, so that the sums so far are seldom
+// scaled. A row's largest weight then lies between 2^kFirst and 2^kMost. fp16 ends at 2^-24: from 2^11
+// on, a weight is off by 2^-36 of the largest at most where fp16's relative steps end (from 1 on it was
+// 2^-25, and tens of thousands of keys far below the largest were lost).
 template <bool kBf16>
 struct Act {
+  static constexpr float kFirst = 11.f, kMost = 15.f;
   typedef _Float16 elem;
   typedef f16x8 x8;
   typedef f16x2 x2;
 };
 template <>
 struct Act<true> {
+  static constexpr float kFirst = 0.f, kMost = 8.f;
   typedef __bf16 elem;
   typedef bf16x8 x8;
   typedef bf16x2 x2;

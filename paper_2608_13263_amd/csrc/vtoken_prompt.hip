@@ -9,8 +9,8 @@
 // serves them all.
 //
 //   out = sum_k w_k V_k / sum_k w_k,  w_k = 2^(x_k - m),  x_k = q . K_k scale log2(e),
-// m a running maximum of the row: where it grows, the sums so far are multiplied by 2^(old - new). The
-// partial sums of splits are joined by the same rule.
+// m a running reference near the row's maximum: where it grows, the sums so far are multiplied by
+// 2^(old - new). The partial sums of splits are joined by the same rule.
 #include <math.h>
 
 #include "vtoken_elements.h"
@@ -413,16 +413,15 @@ void prompt_kernel(PromptArgs a) {
           s[t][e] = seen(key_of(t, e)) ? s[t][e] : -INFINITY;
         }
     }
-    // ---- weights 2^(x - m); m follows the row's maximum where that passes it by 2^8 (the weights
-    // then stay below 2^8, and the sums so far are seldom scaled)
+    // ---- weights 2^(x - m), see Act
     float top = s[0][0];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int e = 0; e < 16; ++e) top = fmaxf(top, s[t][e]);
     top = halves<true>(top) * scale;
-    if (__ballot(top > m + 8.f) != 0) {
-      const float to = top > m ? top : m;
+    if (__ballot(top > m + Act<kBf16>::kMost) != 0) {
+      const float to = fmaxf(top - Act<kBf16>::kFirst, m);
       const float by = to == m ? 1.f : __builtin_amdgcn_exp2f(m - to);
       m = to;
       l *= by;

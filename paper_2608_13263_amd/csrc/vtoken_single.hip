@@ -344,15 +344,15 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
     }
 
     // ---- softmax weights per head (the four lanes of a column share m), powers of two of what a
-    // score is above m; m follows the maximum where that passes it by 2^8
+    // score is above m (see Act)
     float top = sc[0][0];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int j = 0; j < 4; ++j) top = fmaxf(top, sc[t][j]);
     top = groups_reduce<true>(top) * scale;
-    if (__ballot(top > m + 8.f) != 0) {
-      const float next = top > m ? top : m;
+    if (__ballot(top > m + Act<kBf16>::kMost) != 0) {
+      const float next = fmaxf(top - Act<kBf16>::kFirst, m);
       const float f = next == m ? 1.f : __builtin_amdgcn_exp2f(m - next);
       m = next;
       l *= f;
@@ -735,8 +735,8 @@ void shared_kernel(PromptArgs a, int split_tokens, int splits) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) top = fmaxf(top, sc[t][j]);
     top = groups_reduce<true>(top) * scale;
-    if (__ballot(top > m + 8.f) != 0) {
-      const float next = top > m ? top : m;
+    if (__ballot(top > m + Act<kBf16>::kMost) != 0) {
+      const float next = fmaxf(top - Act<kBf16>::kFirst, m);
       const float f = next == m ? 1.f : __builtin_amdgcn_exp2f(m - next);
       m = next;
       l *= f;
@@ -1029,8 +1029,8 @@ void codes_kernel(PromptArgs a, int split_tokens, int splits) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) top = fmaxf(top, sc[t][j]);
     top = groups_reduce<true>(top) * scale;
-    if (__ballot(top > m + 8.f) != 0) {
-      const float next = top > m ? top : m;
+    if (__ballot(top > m + Act<true>::kMost) != 0) {
+      const float next = fmaxf(top - Act<true>::kFirst, m);
       const float f = next == m ? 1.f : __builtin_amdgcn_exp2f(m - next);
       m = next;
       l *= f;
