@@ -540,7 +540,7 @@ vtoken_status vtoken_read_kv(const vtoken_cache* cache, const vtoken_kv_read* re
  * ranks counted in the mapping's order, over the live tokens only. Query head qh reads KV head
  * qh / (num_q_heads / num_kv_heads). out = softmax(scale * q . K^T) @ V, sums and softmax in
  * float32, weights in dtype for the product with V (fp16: to 2^-36 of the row's largest at the
- * finest), rounded once to dtype; a query that sees nothing (ql > n), or whose scores are all
+ * finest; bf16 with max_queries 1: as two parts, to 2^-15), rounded once to dtype; a query that sees nothing (ql > n), or whose scores are all
  * -infinity, gives zeros. Rows of q past the last query are neither read nor written.
  * A query that sees a slot outside the pool gives NaN, no such slot is dereferenced. A request
  * whose slot range is malformed (negative start or count), which holds more than max_tokens slots

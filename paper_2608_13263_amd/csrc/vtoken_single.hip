@@ -71,6 +71,32 @@ __device__ __forceinline__ f32x4 mfma16(u32x4 x, u32x4 y, f32x4 acc) {
   }
 }
 
+// Two weights as 16-bit operands. bf16 takes them in two parts each, off by 2^-15 of a weight (one part
+// by 2^-8, which showed in the output as much as its own rounding): the upper bits, cut off, so that no
+// part is negative, and the rest; where V may hold infinities (kInfinities), the rest is 2^-20 of the
+// weight at least, so that none of them is multiplied by zero. 16- and 8-bit rows pay 0 to 2% for the
+// second part, 4-bit rows 1 to 4%. fp16 takes a weight once rounded, half a step of 2^-11.
+struct Weights {
+  uint32_t hi, lo;
+};
+template <bool kBf16, bool kInfinities>
+__device__ __forceinline__ Weights weights_of(float x, float y) {
+  Weights w{0, 0};
+  if constexpr (kBf16) {
+    const uint32_t u = __float_as_uint(x), v = __float_as_uint(y);
+    w.hi = __builtin_amdgcn_perm(v, u, 0x07060302);
+    float p = x - __uint_as_float(u & 0xffff0000u), q = y - __uint_as_float(v & 0xffff0000u);
+    if (kInfinities) {
+      p = fmaxf(p, x * 0x1p-20f);
+      q = fmaxf(q, y * 0x1p-20f);
+    }
+    w.lo = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(p), static_cast<__bf16>(q)});
+  } else {
+    w.hi = __builtin_bit_cast(uint32_t, f16x2{static_cast<_Float16>(x), static_cast<_Float16>(y)});
+  }
+  return w;
+}
+
 // Combined with the values of lanes i ^ 16, i ^ 32 and i ^ 48.
 template <bool kMax>
 __device__ __forceinline__ float groups_reduce(float x) {
@@ -139,8 +165,7 @@ __device__ __forceinline__ void merge_waves(const PromptArgs& a, float* mrg, flo
 // Wave w takes a round's tokens w kIT .. on; the waves share nothing until the end, so that no barrier
 // stands between a load and its use, and each has a round of K and of V (4 KiB each) in flight. The query
 // heads of the KV head are the 16 columns of the products: K and V are read once for all of them.
-// Weights are rounded to the activations' type for the product, half a step each; the sum is that of the
-// weights before it.
+// The sum of the weights is that before they become operands (weights_of).
 //
 // Bound: HBM. 64 requests, a window of 2,048 and 4 sinks, 8 KV heads of 128, 16 bits, 539 MB: 94 us,
 // 5.7 TB/s (with the merge 100.6), where a copy of 4 GiB moves 4.7 and reads alone up to 7.2. Loads that
@@ -394,12 +419,21 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
           __builtin_amdgcn_sched_barrier(0);
         }
       }
-      // P operand: tokens 4*grp..+3 of tile 2kc, then of tile 2kc+1
-      typename Act<kBf16>::x8 w;
+      // P operand: tokens 4*grp..+3 of tile 2kc, then of tile 2kc+1; where there is one tile, its
+      // weights' lower parts, by the same V rows
+      u32x4 w = {0, 0, 0, 0}, w_lo = {0, 0, 0, 0};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int tile = 2 * kc + (j >> 2);
-        w[j] = static_cast<Elem>(tile < kTiles ? sc[tile < kTiles ? tile : 0][j & 3] : 0.f);
+      for (int j = 0; j < 4; ++j) {
+        const int tile = 2 * kc + j / 2;
+        if (tile >= kTiles) continue;
+        const f32x4 p = sc[tile < kTiles ? tile : 0];
+        const Weights x = weights_of<kBf16, kKind == 1>(p[j % 2 * 2], p[j % 2 * 2 + 1]);
+        w[j] = x.hi;
+        if (kTiles > 1) {
+          w_lo[j] = x.lo;
+        } else {
+          w[j + 2] = x.lo;
+        }
       }
       // V operand rows: lane 16*grp + rho supplies the row of token 4*grp + rho/4 of the first
       // tile (then of the second), elements 4*(rho%4)..+3 of the 16-element chunk
@@ -408,10 +442,11 @@ void single_kernel(PromptArgs a, int split_tokens, int splits) {
 #pragma unroll
       for (int dc = 0; dc < kDC; ++dc) {
         const i16x4 x1 = lds_read_tr16(win + (r1 ^ (dc << 5)));
-        i16x4 x2 = {0, 0, 0, 0};
+        i16x4 x2 = kBf16 ? x1 : i16x4{0, 0, 0, 0};
         if constexpr (kTiles > 1) x2 = lds_read_tr16(win + (r1 ^ (dc << 5)) + 16 * kRowV);
         const i16x8 xv = {x1[0], x1[1], x1[2], x1[3], x2[0], x2[1], x2[2], x2[3]};
-        o[dc] = mfma16<kBf16>(__builtin_bit_cast(u32x4, xv), __builtin_bit_cast(u32x4, w), o[dc]);
+        o[dc] = mfma16<kBf16>(__builtin_bit_cast(u32x4, xv), w, o[dc]);
+        if (kBf16 && kTiles > 1) o[dc] = mfma16<kBf16>(__builtin_bit_cast(u32x4, xv), w_lo, o[dc]);
       }
     }
   };
@@ -548,7 +583,6 @@ __attribute__((amdgpu_waves_per_eu(
     kD > 128 || shared_lds_bytes(kKind, kD, kHeads) > 160 * 1024 / 3 ? 2 : 3)))
 void shared_kernel(PromptArgs a, int split_tokens, int splits) {
   using Elem = typename Act<kBf16>::elem;
-  typedef Elem Elem4 __attribute__((ext_vector_type(4)));
   constexpr int kRow = head_bytes(kKind, kD);        // bytes of a head's row
   constexpr int kIT = wave_tokens(kKind, kD);        // tokens of a wave in a round
   constexpr int kTG = kWaves / kHeads;               // waves of a head
@@ -744,17 +778,17 @@ void shared_kernel(PromptArgs a, int split_tokens, int splits) {
       for (int dc = 0; dc < kDC; ++dc) o[dc] *= f;
     }
     const float base = m == -INFINITY ? 0.f : m;
-    i16x4 w[kTiles];
+    i16x4 w[kTiles], w_lo[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      Elem4 x;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][j], scale, -base));
-        l += p;
-        x[j] = static_cast<Elem>(p);
+        sc[t][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][j], scale, -base));
+        l += sc[t][j];
       }
-      w[t] = __builtin_bit_cast(i16x4, x);
+      const Weights x = weights_of<kBf16, kKind == 1>(sc[t][0], sc[t][1]), y = weights_of<kBf16, kKind == 1>(sc[t][2], sc[t][3]);
+      w[t] = __builtin_bit_cast(i16x4, u32x2{x.hi, y.hi});
+      w_lo[t] = __builtin_bit_cast(i16x4, u32x2{x.lo, y.lo});
     }
     // ---- O += V^T . P^T, a window of V rows at a time
 #pragma unroll
@@ -791,6 +825,7 @@ void shared_kernel(PromptArgs a, int split_tokens, int splits) {
         for (int dc = 0; dc < kDC; ++dc) {
           const i16x4 x = lds_read_tr16(win + (r1 ^ (dc << 5)) + t * 16 * kD * 2);
           o[dc] = mfma16x16<kBf16>(x, w[y * (kWin / 16) + t], o[dc]);
+          if (kBf16) o[dc] = mfma16x16<kBf16>(x, w_lo[y * (kWin / 16) + t], o[dc]);
         }
     }
   }
@@ -813,7 +848,8 @@ void shared_kernel(PromptArgs a, int split_tokens, int splits) {
 //            tile, zeros in the others, picks that tile.
 //   values   come back from LDS transposed as codes (ds_read_b64_tr_b4: a lane gets one head dim of 16
 //            tokens). They multiply as bf16 without their exponents, which differ from token to
-//            token and so go to the weights: w 2^(e - 127), exact, one set of weights per 32 dims.
+//            token and so go to the weights: w 2^(e - 127), exact, one set of weights (two parts each)
+//            per 32 dims, formed for 32 tokens at a time (for 64 at once the kernel took 12 to 22% more).
 //
 // Bound: HBM and latency. 29 requests of 5,043 to 19,788 tokens, 8 KV heads of 128 with 8 query heads
 // each, 411 MB: 106 us, 3.9 TB/s (113 with the merge; the loads alone 88, the arithmetic alone 46). Widened to bf16 on their way into LDS, V took 48 LDS instructions per 64
@@ -1050,37 +1086,34 @@ void codes_kernel(PromptArgs a, int split_tokens, int splits) {
     const int rho_tok = 16 * (row / 4 % kTiles) + 4 * grp + row % 4;
 #pragma unroll
     for (int p = 0; p < kPieces; ++p) {
-      bf16x8 w[kKC];
-#pragma unroll
-      for (int kc = 0; kc < kKC; ++kc)
-#pragma unroll
-        for (int z = 0; z < 2; ++z) {
-          typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
-          const f32x4 e = *(lds_f32x4*)(scales + (p * kIT + 16 * (2 * kc + z) + 4 * grp) * 4);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) w[kc][4 * z + j] = static_cast<__bf16>(sc[2 * kc + z][j] * e[j]);
-        }
       auto codes = [&](int half) {   // of the piece
         return __builtin_amdgcn_ds_read_tr4_b64_v2i32(
             (lds_i32x2*)(vraw + (wt0 + rho_tok) * kRawV + hw * kRow + p * 16 + half * 8));
       };
-      if constexpr (kKC == 2) {
+      // codes of 8 tokens of head dim `row` of the piece's first 16 (x) and last (y), for each k-step
+      const i32x2 x = codes(kKC == 2 ? 0 : row / 8);
+      const i32x2 y = kKC == 2 ? codes(1) : x;
 #pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const i32x2 x = codes(y);
+      for (int kc = 0; kc < kKC; ++kc) {
+        u32x4 w, w_lo;
 #pragma unroll
-          for (int kc = 0; kc < 2; ++kc) {
-            o[2 * p + y] = mfma16<true>(widen_fp4(static_cast<uint32_t>(x[kc]), 1.f),
-                                        __builtin_bit_cast(u32x4, w[kc]), o[2 * p + y]);
+        for (int z = 0; z < 2; ++z) {
+          typedef __attribute__((address_space(3))) f32x4 lds_f32x4;
+          const f32x4 e =
+              sc[2 * kc + z] * *(lds_f32x4*)(scales + (p * kIT + 16 * (2 * kc + z) + 4 * grp) * 4);
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const Weights u = weights_of<true, false>(e[2 * j], e[2 * j + 1]);
+            w[2 * z + j] = u.hi;
+            w_lo[2 * z + j] = u.lo;
           }
         }
-      } else {
-        const i32x2 x = codes(row / 8);
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          o[2 * p + y] = mfma16<true>(widen_fp4(static_cast<uint32_t>(x[y]), 1.f),
-                                      __builtin_bit_cast(u32x4, w[0]), o[2 * p + y]);
-        }
+        const u32x4 v0 = widen_fp4(static_cast<uint32_t>(kKC == 2 ? x[kc] : x[0]), 1.f);
+        const u32x4 v1 = widen_fp4(static_cast<uint32_t>(kKC == 2 ? y[kc] : x[1]), 1.f);
+        o[2 * p] = mfma16<true>(v0, w, o[2 * p]);
+        o[2 * p + 1] = mfma16<true>(v1, w, o[2 * p + 1]);
+        o[2 * p] = mfma16<true>(v0, w_lo, o[2 * p]);
+        o[2 * p + 1] = mfma16<true>(v1, w_lo, o[2 * p + 1]);
       }
     }
     __syncthreads();   // the round's rows have been read
