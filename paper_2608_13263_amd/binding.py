@@ -790,6 +790,13 @@ def _cache_code(cache: KVCache, kv_dtype) -> int:
     return kv_dtype_code(cache.kv.dtype) if code is None else code
 
 
+def _int32s(bits: int) -> None:
+    """The C structs keep 32 bits of an int and say nothing of the others. `bits`: the arguments,
+    or-ed (a negative one is refused by the call itself)."""
+    if bits >> 31 not in (0, -1):
+        raise ValueError("sizes and counts must fit 32 bits")
+
+
 def _enqueue(fn, where: str, device, stream, *args) -> None:
     """fn(*args, stream) with the tensors' device current, on `stream` or that device's current
     one."""
@@ -820,6 +827,7 @@ def write_kv(cache: KVCache, k, v, slots, layer: int, q=None, positions=None, co
     import torch
     dev = cache.kv.device
     H, D, n, act = cache.num_kv_heads, cache.head_dim, slots.numel(), k.dtype
+    _int32s(layer | n)
     _ints(slots, "slots", dev)
     q_heads = q_stride = out_stride = rotary = num_positions = 0
     if q is not None:
@@ -862,6 +870,7 @@ def read_kv(cache: KVCache, slots, layer: int, dtype=None, k_out=None, v_out=Non
     import torch
     dev = cache.kv.device
     H, D, n = cache.num_kv_heads, cache.head_dim, slots.numel()
+    _int32s(layer | n)
     _ints(slots, "slots", dev)
     code = _cache_code(cache, kv_dtype)
     if dtype is None:
@@ -915,6 +924,7 @@ def paged_attention(cache: KVCache, q, slot_indptr, slots, layer: int, max_token
         _ints(slot_count, "slot_count", dev, R)
     if max_queries is None:
         max_queries = 1 if q_indptr is None else rows
+    _int32s(layer | rows | max_queries | max_tokens | window | sinks)
     a = CAttention(q.data_ptr(), out.data_ptr(), stride,
                    _activation(out, "out", dev, act, heads, D), _ptr(q_indptr), _ptr(slot_count),
                    0, 0, rows, max_queries, max_tokens, heads, cache.num_kv_heads, D, layer,

@@ -244,3 +244,19 @@ def test_most_head_rows():
                        None) == CODE["VTOKEN_ERR_" + code]
         assert _status("vtoken_read_kv", _read(num_tokens=tokens, **r), c,
                        None) == CODE["VTOKEN_ERR_" + code]
+
+
+def test_sizes_past_32_bits_are_refused():
+    """The structs would keep the lower 32 bits: another layer, a window of 5, one of everything."""
+    cache = SimpleNamespace(kv=torch.zeros(2, 1, 16, 2, 64, dtype=torch.bfloat16), num_kv_heads=2,
+                            head_dim=64)
+    x, i = torch.zeros(3, 2, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    for far in (2 ** 31, 2 ** 32, 2 ** 32 + 5, -2 ** 32):
+        with pytest.raises(ValueError, match="32 bits"):
+            B.write_kv(cache, x, x, i, far)
+        with pytest.raises(ValueError, match="32 bits"):
+            B.read_kv(cache, i, far)
+        for kw in (dict(layer=far), dict(max_tokens=far), dict(window=far), dict(sinks=far),
+                   dict(max_queries=far, q_indptr=i)):
+            with pytest.raises(ValueError, match="32 bits"):
+                B.paged_attention(cache, x, i, i, **{"layer": 0, "max_tokens": 5, **kw})
