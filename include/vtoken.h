@@ -454,8 +454,8 @@ vtoken_status vtoken_paged_decode_noalloc(const vtoken_cache* cache,
  * Writing new tokens' K and V into the cache, reading rows back, and attention of a ragged batch
  * of queries over it. Activations (q, k, v, outputs) are fp16 or bf16 (VTOKEN_KV_FP16 or
  * VTOKEN_KV_BF16 in `dtype`) with a stride in elements between tokens, the heads of a token side
- * by side; pointers to them must be aligned to 16 bytes and strides be multiples of 8 elements
- * (VTOKEN_ERR_ARGUMENT otherwise). An fp16 cache takes fp16 activations, a bf16 or 4-bit cache
+ * by side; pointers to them and to the cache must be aligned to 16 bytes and strides be multiples of
+ * 8 elements (VTOKEN_ERR_ARGUMENT otherwise). An fp16 cache takes fp16 activations, a bf16 or 4-bit cache
  * bf16, an fp8 cache either.
  *
  * 4-bit caches (VTOKEN_KV_MXFP4): a row is the codes [num_kv_heads][head_dim / 2] (e2m1: 0, 0.5,

@@ -616,7 +616,8 @@ vtoken_status check_rows(const vtoken_cache* c, int32_t heads, int32_t head_dim,
                                   : kv_dtype != VTOKEN_KV_FP8_E4M3 && dtype != kv_dtype) {
     return VTOKEN_ERR_SHAPE;
   }
-  return VTOKEN_OK;
+  // (rows are multiples of 16 bytes, read and written 16 at a time)
+  return reinterpret_cast<uintptr_t>(c->kv) % 16 != 0 ? VTOKEN_ERR_ARGUMENT : VTOKEN_OK;
 }
 
 // An activation tensor: 16-byte aligned rows of `width` elements that do not overlap.

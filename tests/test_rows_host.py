@@ -260,3 +260,13 @@ def test_sizes_past_32_bits_are_refused():
                    dict(max_queries=far, q_indptr=i)):
             with pytest.raises(ValueError, match="32 bits"):
                 B.paged_attention(cache, x, i, i, **{"layer": 0, "max_tokens": 5, **kw})
+
+
+def test_a_cache_off_16_bytes_is_refused():
+    """A view that starts inside a row's 16 bytes: the kernels read and write 16 at a time."""
+    for off in (2, 8, 15):
+        c = _cache(kv=P + off)
+        for st in (_status("vtoken_write_kv", _write(num_tokens=2), c, None),
+                   _status("vtoken_read_kv", _read(num_tokens=2), c, None),
+                   _status("vtoken_paged_attention", _attention(num_queries=5), c, 2, P, P, None)):
+            assert st == CODE["VTOKEN_ERR_ARGUMENT"]
