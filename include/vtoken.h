@@ -461,9 +461,11 @@ vtoken_status vtoken_paged_decode_noalloc(const vtoken_cache* cache,
  * 4-bit caches (VTOKEN_KV_MXFP4): a row is the codes [num_kv_heads][head_dim / 2] (e2m1: 0, 0.5,
  * 1, 1.5, 2, 3, 4, 6 and a sign in bit 3; even values in the low half of a byte), then the
  * exponents [num_kv_heads][head_dim / 32] (e8m0: value = e2m1 * 2^(e - 127), 255 is NaN; 0 is
- * not written, and stands for zeros), padded to a multiple of 16 bytes. Such a row is moved as it is by every call that moves rows: describe
- * the cache to them as num_kv_heads 1, head_dim vtoken_kv_row_bytes(), elem_bytes 1; the calls
- * below carry the heads and head_dim themselves (for the other types equal to the cache's). */
+ * not written, and stands for zeros; 253 and 254 are not written either, and attention may take
+ * their values, past bf16's range, for infinities or NaN), padded to a multiple of 16 bytes. Such a
+ * row is moved as it is by every call that moves rows: describe the cache to them as num_kv_heads 1,
+ * head_dim vtoken_kv_row_bytes(), elem_bytes 1; the calls below carry the heads and head_dim
+ * themselves (for the other types equal to the cache's). */
 enum { VTOKEN_KV_MXFP4 = 3 };
 
 /* Bytes of one token's row in one plane; -1 for sizes that no call takes (head_dim must be a

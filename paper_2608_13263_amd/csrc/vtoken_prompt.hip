@@ -320,8 +320,8 @@ void prompt_kernel(PromptArgs a) {
 #pragma unroll
         for (int y = 0; y < kOut; ++y) o[y] = u32x4{fill, fill, fill, fill};
       }
-      if (kKind == 3 && look && is_v) {   // (the codes are finite)
-        if (exponent[kKind == 3 ? x : 0] == 255) {
+      if (kKind == 3 && look && is_v) {   // (6 x 2^125 is bf16's last; the codes are finite)
+        if (exponent[kKind == 3 ? x : 0] > 252) {
           odd |= !past && !outside;
 #pragma unroll
           for (int y = 0; y < kOut; ++y) o[y] = u32x4{0, 0, 0, 0};
@@ -485,8 +485,8 @@ void prompt_kernel(PromptArgs a) {
       const uint8_t* row = kplane + a.plane_bytes + (int64_t)slot * a.row_bytes;
 #pragma unroll
       for (int dc = 0; dc < kDC; ++dc)
-        if constexpr (kKind == 3) {   // an exponent's 32 values are NaN, or none
-          if (row[a.num_kv_heads * (kD / 2) + h * (kD / 32) + dc] != 255) continue;
+        if constexpr (kKind == 3) {   // an exponent's 32 values are lost, or none
+          if (row[a.num_kv_heads * (kD / 2) + h * (kD / 32) + dc] <= 252) continue;
 #pragma unroll
           for (int e = 0; e < 16; ++e) o[dc][e] = __builtin_nanf("");
         } else {

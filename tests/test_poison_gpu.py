@@ -83,3 +83,27 @@ def test_prompts(kind, H, G, D, poison):
                 assert torch.equal(lost.all(-1).all(-1), sees)
                 assert torch.equal(lost.any(-1).any(-1), sees)
                 assert bool((out[~sees] == 1).all())
+
+
+@pytest.mark.parametrize("e", [253, 254, 255])
+@pytest.mark.parametrize("H,D,queries", [(2, 64, 90), (1, 128, 30), (4, 32, 1)])
+def test_largest_exponents_that_are_hidden(e, H, D, queries):
+    """4-bit values that bf16 holds as infinities, in V (and K) of a key that some queries do not see."""
+    n, at = 200, 195 if queries > 1 else 20
+    for window, sinks in ((0, 0), (150, 4)):
+        c = Case("mxfp4", H, 4, D, [n], [queries], seed=31)
+        kw = dict(q_indptr=None, max_queries=1) if queries == 1 else {}
+        clean = c.run(window, sinks, **kw)[:queries].cpu()
+        rows = S.bytes_of(c.cache).clone()
+        for plane in (2, 3):
+            row = rows[plane][int(c.slots[at])]
+            row[: H * D // 2] = 0x7F    # 6 and -6
+            row[H * D // 2: H * D // 2 + H * D // 32] = e
+        c.cache.kv.view(torch.uint8).reshape(rows.shape).copy_(rows)
+        out = c.run(window, sinks, **kw)[:queries].cpu()
+        p = torch.arange(n - queries, n)
+        sees = (p >= at) & (((p - window) < at) | (at < sinks) if window else True)
+        if e == 255:   # (6 x 2^126 and more are numbers, which a weight of zero leaves out)
+            assert not bool(torch.isfinite(out[sees]).any())
+        assert bool(((out[~sees].double() - clean[~sees].double()).abs() <= 4 * S.HALF_STEP["bf16"]
+                     * float(clean.abs().max())).all())
