@@ -282,6 +282,12 @@ def _empty(shape, dtype, device, stream):
     return x
 
 
+def _on(stream):
+    """torch.empty's place in a call on a given stream."""
+    return lambda *shape, dtype, device: _empty(shape if len(shape) > 1 else shape[0], dtype, device,
+                                                stream)
+
+
 class _Cached:
     """The C struct of an object is built once and reused (it only holds the tensors' device
     addresses and sizes); assigning any attribute drops it. Building the structs costs a few
@@ -402,7 +408,8 @@ class Plan(_Cached):
         R, T, M, f = batch.num_reqs, batch.num_tokens, batch.num_bt_entries, batch.free_len
 
         def e(n):
-            return _empty(max(int(n), 1), torch.int32, device, stream)
+            return empty(max(int(n), 1), dtype=torch.int32, device=device)
+        empty = torch.empty if stream is None else _on(stream)
         rows = M if inplace else min(f, M)
         return cls(token_slot=e(T), live_count=e(R), admitted=e(R), dst_indptr=e(R + 1),
                    new_bt_indptr=e(R + 1), new_block_ids=e(M),
@@ -497,9 +504,10 @@ def check_layout(cache: KVCache, batch: Batch, workspace=None, stream=None):
     import torch
     lib = load_library()
     need = int(lib.vtoken_check_layout_workspace_bytes(cache.num_blocks))
+    empty = torch.empty if stream is None else _on(stream)
     if workspace is None:
-        workspace = _empty(max(need // 4, 1), torch.int32, cache.kv.device, stream)
-    status = _empty(1, torch.int32, cache.kv.device, stream)
+        workspace = empty(max(need // 4, 1), dtype=torch.int32, device=cache.kv.device)
+    status = empty(1, dtype=torch.int32, device=cache.kv.device)
     c, b = cache.c(), batch.c()
     _check(lib.vtoken_check_layout(ctypes.byref(c), ctypes.byref(b), _ptr(workspace),
                                    int(workspace.numel() * workspace.element_size()),
@@ -532,10 +540,11 @@ def build_slot_mapping(batch: Batch, plan: Plan, slot_indptr=None, slots=None,
     import torch
     lib = load_library()
     dev = plan.counters.device
+    empty = torch.empty if stream is None else _on(stream)
     if slot_indptr is None:
-        slot_indptr = _empty(batch.num_reqs + 1, torch.int32, dev, stream)
+        slot_indptr = empty(batch.num_reqs + 1, dtype=torch.int32, device=dev)
     if slots is None:
-        slots = _empty(max(batch.num_tokens, 1), torch.int32, dev, stream)
+        slots = empty(max(batch.num_tokens, 1), dtype=torch.int32, device=dev)
     b, p = batch.c(), plan.c()
     _check(lib.vtoken_build_slot_mapping(ctypes.byref(b), ctypes.byref(p), _ptr(slot_indptr),
                                          _ptr(slots), int(slots.numel()), _stream(stream)),
@@ -550,9 +559,10 @@ def build_slot_table(batch: Batch, plan: Plan, reserve: int, stream=None):
     lib = load_library()
     dev = plan.counters.device
     R = batch.num_reqs
-    start = _empty(R + 1, torch.int32, dev, stream)
-    count = _empty(max(R, 1), torch.int32, dev, stream)
-    slots = _empty(max(batch.num_tokens + R * int(reserve), 1), torch.int32, dev, stream)
+    empty = torch.empty if stream is None else _on(stream)
+    start = empty(R + 1, dtype=torch.int32, device=dev)
+    count = empty(max(R, 1), dtype=torch.int32, device=dev)
+    slots = empty(max(batch.num_tokens + R * int(reserve), 1), dtype=torch.int32, device=dev)
     b, p = batch.c(), plan.c()
     _check(lib.vtoken_build_slot_table(ctypes.byref(b), ctypes.byref(p), int(reserve),
                                        _ptr(start), _ptr(count), _ptr(slots),
@@ -568,7 +578,8 @@ def append_slots(slot_start, slot_count, slots, append_indptr, append_slots, sta
     import torch
     lib = load_library()
     if status is None:
-        status = _empty(1, torch.int32, slots.device, stream)
+        status = (torch.empty if stream is None else _on(stream))(1, dtype=torch.int32,
+                                                                  device=slots.device)
     R = int(append_indptr.numel()) - 1
     most = 0 if append_slots is None else int(append_slots.numel())
     _check(lib.vtoken_append_slots_n(R, most, _ptr(append_indptr), _ptr(append_slots),
@@ -610,13 +621,14 @@ def paged_decode(cache: KVCache, q, slot_indptr, slots, layer: int, max_tokens: 
     R, Hq, D = (int(x) for x in q.shape)
     if D != cache.head_dim:
         raise ValueError("q head_dim differs from the cache's")
+    empty = torch.empty if stream is None else _on(stream)
     if out is None:
-        out = _empty(q.shape, torch.float32, q.device, stream)
+        out = empty(q.shape, dtype=torch.float32, device=q.device)
     if out.shape != q.shape or out.dtype != torch.float32 or not out.is_contiguous():
         raise ValueError("out must match q")
     need = decode_workspace_bytes(R, Hq, D, max_tokens)
     if workspace is None:
-        workspace = _empty(max(need // 4, 1), torch.float32, q.device, stream)
+        workspace = empty(max(need // 4, 1), dtype=torch.float32, device=q.device)
     code = kv_dtype_code(cache.kv.dtype) if kv_dtype is None else int(kv_dtype)
     if scale is None:
         scale = D ** -0.5
@@ -691,7 +703,8 @@ class PlannerState:
         import torch
 
         def e(n, dt=torch.int32):
-            return _empty(max(int(n), 1), dt, device, stream)
+            return empty(max(int(n), 1), dtype=dt, device=device)
+        empty = torch.empty if stream is None else _on(stream)
         M, R = batch.num_bt_entries, batch.num_reqs
         if pinned is not None and not isinstance(pinned, torch.Tensor):
             import numpy as np
@@ -790,7 +803,7 @@ def _cache_code(cache: KVCache, kv_dtype) -> int:
     return kv_dtype_code(cache.kv.dtype) if code is None else code
 
 
-def _int32s(bits: int) -> None:
+def _refuse_past_32_bits(bits: int) -> None:
     """The C structs keep 32 bits of an int and say nothing of the others. `bits`: the arguments,
     or-ed (a negative one is refused by the call itself)."""
     if bits >> 31 not in (0, -1):
@@ -827,14 +840,15 @@ def write_kv(cache: KVCache, k, v, slots, layer: int, q=None, positions=None, co
     import torch
     dev = cache.kv.device
     H, D, n, act = cache.num_kv_heads, cache.head_dim, slots.numel(), k.dtype
-    _int32s(layer | n)
+    if (layer | n) >> 31:
+        _refuse_past_32_bits(layer | n)
     _ints(slots, "slots", dev)
     q_heads = q_stride = out_stride = rotary = num_positions = 0
     if q is not None:
         q_heads = int(q.shape[1]) if q.dim() == 3 else 0
         q_stride = _activation(q, "q", dev, act, q_heads, D, n)
         if q_out is None:
-            q_out = _empty(q.shape, act, dev, stream)
+            q_out = (torch.empty if stream is None else _on(stream))(q.shape, dtype=act, device=dev)
         out_stride = _activation(q_out, "q_out", dev, act, q_heads, D, n)
     elif q_out is not None:
         raise ValueError("q_out without q")
@@ -870,16 +884,18 @@ def read_kv(cache: KVCache, slots, layer: int, dtype=None, k_out=None, v_out=Non
     import torch
     dev = cache.kv.device
     H, D, n = cache.num_kv_heads, cache.head_dim, slots.numel()
-    _int32s(layer | n)
+    if (layer | n) >> 31:
+        _refuse_past_32_bits(layer | n)
     _ints(slots, "slots", dev)
     code = _cache_code(cache, kv_dtype)
     if dtype is None:
         dtype = k_out.dtype if k_out is not None else \
             torch.float16 if code == KV_FP16 else torch.bfloat16
+    empty = torch.empty if stream is None else _on(stream)
     if k_out is None:
-        k_out = _empty((n, H, D), dtype, dev, stream)
+        k_out = empty(n, H, D, dtype=dtype, device=dev)   # (a tuple costs 0.4 us more)
     if v_out is None:
-        v_out = _empty((n, H, D), dtype, dev, stream)
+        v_out = empty(n, H, D, dtype=dtype, device=dev)
     r = CKVRead(slots.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
                 _activation(k_out, "k_out", dev, dtype, H, D, n),
                 _activation(v_out, "v_out", dev, dtype, H, D, n), n, H, D, layer,
@@ -914,8 +930,9 @@ def paged_attention(cache: KVCache, q, slot_indptr, slots, layer: int, max_token
     _ints(slots, "slots", dev)
     R, rows = slot_indptr.numel() - 1, int(q.shape[0])
     stride = _activation(q, "q", dev, act, heads, D)
+    empty = torch.empty if stream is None else _on(stream)
     if out is None:
-        out = _empty(q.shape, act, dev, stream)
+        out = empty(q.shape, dtype=act, device=dev)
     elif out.shape != q.shape:
         raise ValueError("out must match q")
     if q_indptr is not None:
@@ -924,7 +941,9 @@ def paged_attention(cache: KVCache, q, slot_indptr, slots, layer: int, max_token
         _ints(slot_count, "slot_count", dev, R)
     if max_queries is None:
         max_queries = 1 if q_indptr is None else rows
-    _int32s(layer | rows | max_queries | max_tokens | window | sinks)
+    bits = layer | rows | max_queries | max_tokens | window | sinks
+    if bits >> 31:
+        _refuse_past_32_bits(bits)
     a = CAttention(q.data_ptr(), out.data_ptr(), stride,
                    _activation(out, "out", dev, act, heads, D), _ptr(q_indptr), _ptr(slot_count),
                    0, 0, rows, max_queries, max_tokens, heads, cache.num_kv_heads, D, layer,
@@ -934,7 +953,7 @@ def paged_attention(cache: KVCache, q, slot_indptr, slots, layer: int, max_token
     ref = ctypes.byref(a)
     need = lib.vtoken_attention_workspace_bytes(ref, R)   # (-1: the call itself says why)
     if workspace is None and need > 0:
-        workspace = _empty((need + 3) // 4, torch.float32, dev, stream)
+        workspace = empty((need + 3) // 4, dtype=torch.float32, device=dev)
     if workspace is not None:
         if workspace.device != dev or not workspace.is_contiguous():
             raise ValueError(f"workspace must be contiguous on {dev}")
