@@ -131,20 +131,24 @@ __device__ __forceinline__ uint32_t only_finite(uint32_t w) {
 // operand of O^T = V^T P^T: no score goes through LDS. K and V of 16 bits go from memory to LDS without
 // registers, a step ahead; V is read transposed.
 // Weights are rounded to the activations' type for the product, half a step each; the sum is that of the
-// rounded ones, and the output is rounded once.
+// rounded ones, and the output is rounded once. In two parts, as single tokens' weights are, they would be
+// off by 2^-15 of themselves instead of 2^-8, for 576 us instead of 443 (16 bits), 476 instead of 373
+// (8 bits) and 52 instead of 45 (4 bits, few queries of many keys): not taken.
 //
 // Measured: 8,192 queries with a window of 4,096, 32 query and 8 KV heads of 128, 16 bits, 412.6 GFLOP:
-// 447 us, 924 TFLOP/s, three quarters of a large library product's 1,202. Counters: matrix cores busy
-// 42% of the time, vector instructions 47%, LDS 22% without conflicts, at 2.08 GHz; HBM idle. Without the
-// exponentials, or with half of the V reads, it takes 3 to 5% less, without the loads 15: none of them
-// is the bound, the order within a wave and the clock under this load are.
+// 443 to 468 us on different cards, 880 to 930 TFLOP/s, three quarters of a large library product's 1,202 to
+// 1,215. Counters: matrix cores busy 44% of the time, vector instructions 51%, LDS 23% without conflicts;
+// HBM idle. In an earlier version, without the exponentials or with half of the V reads it took 3 to 5%
+// less, without the loads 15: none of them was the bound, the order within a wave and the clock under this
+// load were.
 // Measured and not kept: 64 rows by 32 keys a wave, which halves the reads of LDS (2,048 queries of 4,096
 // keys 180 us instead of 138, 26 registers spilled; one workgroup per CU, none spilled, 209; 64 dims 90.5
-// instead of 88); scores a step ahead of the weights (16 bits of 128 dims 2 to 7% faster, 8 bits 1% and
-// 64 dims 4% slower).
+// instead of 88); scores a step ahead of the weights (16 bits of 128 dims 2 to 7% faster where a request
+// has 8,192 keys and no window, the same at the size above; 8 bits 1% and 64 dims 4% slower).
 //
-// (Two workgroups per CU also at 256 dims, where that spills 8 to 22 registers: 4,096 queries of 8,192
-// keys, 4 KV heads with 2 query heads each, take 349 us instead of 485 in fp8, 308 instead of 401 in 4 bits.)
+// (Two workgroups per CU also at 256 dims, where that spills registers: 4,096 queries of 8,192 keys, 4 KV
+// heads with 2 query heads each, take 349 to 355 us instead of 485 in fp8, 308 to 323 instead of 401 in
+// 4 bits.)
 template <bool kBf16, int kKind, int kD>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(2)))
@@ -582,8 +586,8 @@ void prompt_kernel(PromptArgs a) {
 }
 
 // Merges the split records (m, l, O) of a tile's rows, a row per wave: weights 2^(m_s - max m).
-// Bound: latency; every wave reads all the (m_s, l_s) at once and eight records at a time. 976 rows of
-// 64 records of 128 dims: 11.6 us (32 MB, 2.8 TB/s); a workgroup with its rows one after another took 128.
+// Bound: latency; every wave reads all the (m_s, l_s) at once and eight records at a time. 768 rows of
+// 64 records of 128 dims: 10.5 us (25.6 MB, 2.4 TB/s); a workgroup with its rows one after another took 128.
 template <bool kBf16>
 __global__ __launch_bounds__(kThreads) void combine_kernel(PromptArgs a, int splits) {
   using Elem = typename Act<kBf16>::elem;
@@ -656,7 +660,8 @@ int64_t most_tiles(const PromptArgs& a) {
 // keys are many (16 queries of 32,768 keys 55 us instead of 48, 4 x 64 of 8,192 93 instead of 71), more
 // than that run one after another (4 x 64 of 8,192: 86 us with 768). A split of fewer than eight steps
 // costs more to merge than it saves (512 queries of 512 keys: 31 us at four steps or more, 23 at eight);
-// sixteen leave too few (128 queries of 4,096 keys 44 us instead of 32).
+// sixteen leave too few (128 queries of 4,096 keys 44 us instead of 32). (Measured before the kernel's last
+// steps: as kept, the sizes of one request take 44, 20 and 28 us now.)
 int prompt_splits(const PromptArgs& a) {
   const int64_t groups = most_tiles(a) * a.num_kv_heads;
   if (groups == 0) return 1;

@@ -8,11 +8,13 @@
 // its row with one load per lane, reduces and turns it in registers and stores it: every byte is
 // moved once. A group takes kRowsPer rows of a token one after the other: their loads are in flight
 // together, and the angles, the weights and the token's slot and position are read once for them.
-// Both are bound by HBM where the calls are large and by latency where they are small: 8,192 tokens of 32
-// query and 8 KV heads of 128 into a 16-bit cache (206 MB) take 44 us, 4.6 TB/s, as a copy of 4 GiB does
-// (4.7); 4,097 tokens of 64 query heads into a 4-bit cache (158 MB) 39 us, 4.0 TB/s; 65,536 tokens' 4-bit
-// rows read (340 MB) 66 us, 5.1 TB/s; one token 4.2 us. With one head row to a group the first took 70 us
-// and the last but one 96; with four of mixed kinds the first took 54.
+// Large calls move at the rate of a library's copy of 4 GiB (4.7 TB/s), which is not the memory's: probes
+// on this card read at 7.2 TB/s, write at 6.1 and copy at 6.2. Small ones are bound by latency. 8,192 tokens
+// of 32 query and 8 KV heads of 128 into a 16-bit cache (206 MB, half of them written) take 44 us, 4.6 TB/s,
+// where those rates give 31; 4,097 tokens of 64 query heads into a 4-bit cache (158 MB) 38 us, 4.1 TB/s;
+// 65,536 tokens' 4-bit rows read (340 MB, four fifths written) 66 us, 5.1 TB/s, where the rates give 54; one
+// token 4 us. With one head row to a group the first took 70 us and the last but one 96; with four of mixed
+// kinds the first took 54.
 #include "vtoken_elements.h"
 
 namespace vtoken {

@@ -167,8 +167,8 @@ __device__ __forceinline__ void merge_waves(const PromptArgs& a, float* mrg, flo
 // heads of the KV head are the 16 columns of the products: K and V are read once for all of them.
 // The sum of the weights is that before they become operands (weights_of).
 //
-// Bound: HBM. 64 requests, a window of 2,048 and 4 sinks, 8 KV heads of 128, 16 bits, 539 MB: 94 us,
-// 5.7 TB/s (with the merge 100.6), where a copy of 4 GiB moves 4.7 and reads alone up to 7.2. Loads that
+// Bound: HBM. 64 requests, a window of 2,048 and 4 sinks, 8 KV heads of 128, 16 bits, 539 MB: 95 us,
+// 5.7 TB/s (with the merge 100.6, 5.4), where reads alone reach 7.2. Loads that
 // leave the caches alone (nontemporal) are for rows that no other workgroup reads.
 template <bool kBf16, int kKind, int kD>
 __global__ __launch_bounds__(kThreads)
@@ -572,8 +572,8 @@ constexpr int shared_lds_bytes(int kind, int head_dim, int heads) {
          kWaves * shared_window(kind, head_dim) * head_dim * 2;
 }
 
-// Head rows of less than a line (an 8-bit head of 64 dims, 8 KV heads, 32 requests of 4,096 tokens: 38 us,
-// 3.5 TB/s, where single_kernel's pieces of half lines take 54; a 16-bit head of 32 dims 34 instead of 52;
+// Head rows of less than a line (an 8-bit head of 64 dims, 8 KV heads, 32 requests of 4,096 tokens: 37 us,
+// 3.7 TB/s, where single_kernel's pieces of half lines take 54; a 16-bit head of 32 dims 33 instead of 52;
 // with one KV head, or few tokens, both take the same). Wave w takes head w % kHeads of the workgroup's kHeads, and of a
 // round's tokens the (w / kHeads)-th kIT; the workgroup loads the round's rows together, whole lines
 // of all its heads at a time, and passes them through LDS as they are stored.
@@ -852,9 +852,10 @@ void shared_kernel(PromptArgs a, int split_tokens, int splits) {
 //            per 32 dims, formed for 32 tokens at a time (for 64 at once the kernel took 12 to 22% more).
 //
 // Bound: HBM and latency. 29 requests of 5,043 to 19,788 tokens, 8 KV heads of 128 with 8 query heads
-// each, 411 MB: 106 us, 3.9 TB/s (113 with the merge; the loads alone 88, the arithmetic alone 46). Widened to bf16 on their way into LDS, V took 48 LDS instructions per 64
-// tokens of 128 dims instead of 24, and K 64 conversions instead of none; with each wave loading for
-// itself, its 64-byte pieces and 4-byte exponents came in at 3.5 TB/s with nothing else to do.
+// each, 411 MB: 105 to 108 us, 3.9 TB/s (112 to 114 with the merge, 3.6; with weights of one part the loads
+// alone took 88 and the arithmetic alone 46). Widened to bf16 on their way into LDS, V took 48 LDS
+// instructions per 64 tokens of 128 dims instead of 24, and K 64 conversions instead of none; with each wave
+// loading for itself, its 64-byte pieces and 4-byte exponents came in at 3.5 TB/s with nothing else to do.
 template <int kD, int kHeads>
 __global__ __launch_bounds__(kThreads)
 __attribute__((amdgpu_waves_per_eu(kD > 128 ? 2 : 3)))
