@@ -265,10 +265,11 @@ def _stream(stream) -> int:
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
 
 
-def _empty(shape, dtype, device, stream):
+def _empty(shape, dtype, device, stream, keep=True):
     """Memory that a call on `stream` writes. Given a stream, it comes from that stream's own: a block
     of the current stream's may have work of its last owner still to come, which the call would not
-    wait for. It is not handed out again before the current stream has done with it either."""
+    wait for. It is not handed out again before the current stream has done with it either, but for a
+    workspace (keep False), which no other stream touches."""
     import torch
     if stream is None:
         return torch.empty(shape, dtype=dtype, device=device)
@@ -278,14 +279,15 @@ def _empty(shape, dtype, device, stream):
             torch.cuda.default_stream(device)
     with torch.cuda.stream(stream):
         x = torch.empty(shape, dtype=dtype, device=device)
-    x.record_stream(torch.cuda.current_stream(device))
+    if keep:
+        x.record_stream(torch.cuda.current_stream(device))
     return x
 
 
-def _on(stream):
+def _on(stream, keep=True):
     """torch.empty's place in a call on a given stream."""
     return lambda *shape, dtype, device: _empty(shape if len(shape) > 1 else shape[0], dtype, device,
-                                                stream)
+                                                stream, keep)
 
 
 class _Cached:
@@ -504,9 +506,10 @@ def check_layout(cache: KVCache, batch: Batch, workspace=None, stream=None):
     import torch
     lib = load_library()
     need = int(lib.vtoken_check_layout_workspace_bytes(cache.num_blocks))
-    empty = torch.empty if stream is None else _on(stream)
     if workspace is None:
+        empty = torch.empty if stream is None else _on(stream, False)
         workspace = empty(max(need // 4, 1), dtype=torch.int32, device=cache.kv.device)
+    empty = torch.empty if stream is None else _on(stream)
     status = empty(1, dtype=torch.int32, device=cache.kv.device)
     c, b = cache.c(), batch.c()
     _check(lib.vtoken_check_layout(ctypes.byref(c), ctypes.byref(b), _ptr(workspace),
@@ -628,6 +631,7 @@ def paged_decode(cache: KVCache, q, slot_indptr, slots, layer: int, max_tokens: 
         raise ValueError("out must match q")
     need = decode_workspace_bytes(R, Hq, D, max_tokens)
     if workspace is None:
+        empty = torch.empty if stream is None else _on(stream, False)
         workspace = empty(max(need // 4, 1), dtype=torch.float32, device=q.device)
     code = kv_dtype_code(cache.kv.dtype) if kv_dtype is None else int(kv_dtype)
     if scale is None:
@@ -953,6 +957,7 @@ def paged_attention(cache: KVCache, q, slot_indptr, slots, layer: int, max_token
     ref = ctypes.byref(a)
     need = lib.vtoken_attention_workspace_bytes(ref, R)   # (-1: the call itself says why)
     if workspace is None and need > 0:
+        empty = torch.empty if stream is None else _on(stream, False)
         workspace = empty((need + 3) // 4, dtype=torch.float32, device=dev)
     if workspace is not None:
         if workspace.device != dev or not workspace.is_contiguous():

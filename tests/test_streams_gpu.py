@@ -138,3 +138,32 @@ def test_a_pass_and_what_reads_it():
     for side, given in _streams():
         for a, b in zip(run(given), want):
             assert torch.equal(a, b)
+
+
+def test_captured_on_another_stream():
+    """Calls on a side stream that a capture forks to, their outputs and workspaces made there: every
+    replay is the eager result, with eager calls between them."""
+    c = Case("bf16", 2, 4, 128, [6000], [1], seed=43, extra=0)
+    q, slots = c.q.cuda(), c.slots.cuda()
+    indptr = torch.tensor(c.indptr, dtype=torch.int32).cuda()
+    side = torch.cuda.Stream()
+
+    def call(stream=None):
+        out = B.paged_attention(c.cache, q, indptr, slots, 1, 6000, stream=stream)
+        return B.paged_attention(c.cache, out, indptr, slots, 1, 6000, stream=stream), out
+
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        side.wait_stream(torch.cuda.current_stream())
+        got = call(side)
+        torch.cuda.current_stream().wait_stream(side)
+    for i in range(4):
+        q.copy_(torch.randn(q.shape, generator=torch.Generator().manual_seed(i)))
+        want = call()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        call(side)
+        torch.cuda.synchronize()

@@ -50,3 +50,11 @@ def test_memory_of_the_stream_that_writes_it(streams):
     B._empty(4, torch.int32, "cuda", 0)     # the handle of the default stream
     assert streams["at"] == ["current", 7, 11, "default"]
     assert streams["kept"] == ["current"] * 3
+
+
+def test_workspaces_are_the_streams_own(streams):
+    """No other stream touches a workspace: the next call on its stream may have it at once."""
+    B._on(streams["Stream"](7), False)(3, 2, dtype=torch.float32, device="cuda")
+    assert streams["at"] == [7] and streams["kept"] == []
+    B._on(streams["Stream"](7))(5, dtype=torch.float32, device="cuda")
+    assert streams["at"] == [7, 7] and streams["kept"] == ["current"]
