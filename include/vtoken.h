@@ -455,8 +455,8 @@ vtoken_status vtoken_paged_decode_noalloc(const vtoken_cache* cache,
  * of queries over it. Activations (q, k, v, outputs) are fp16 or bf16 (VTOKEN_KV_FP16 or
  * VTOKEN_KV_BF16 in `dtype`) with a stride in elements between tokens, the heads of a token side
  * by side; pointers to them and to the cache must be aligned to 16 bytes and strides be multiples of
- * 8 elements (VTOKEN_ERR_ARGUMENT otherwise). An fp16 cache takes fp16 activations, a bf16 or 4-bit cache
- * bf16, an fp8 cache either.
+ * 8 elements (VTOKEN_ERR_ARGUMENT otherwise). An fp16 cache takes fp16 activations, a bf16 or 4-bit
+ * cache bf16, an fp8 cache either.
  *
  * 4-bit caches (VTOKEN_KV_MXFP4): a row is the codes [num_kv_heads][head_dim / 2] (e2m1: 0, 0.5,
  * 1, 1.5, 2, 3, 4, 6 and a sign in bit 3; even values in the low half of a byte), then the
@@ -542,8 +542,9 @@ vtoken_status vtoken_read_kv(const vtoken_cache* cache, const vtoken_kv_read* re
  * ranks counted in the mapping's order, over the live tokens only. Query head qh reads KV head
  * qh / (num_q_heads / num_kv_heads). out = softmax(scale * q . K^T) @ V, sums and softmax in
  * float32, weights in dtype for the product with V (fp16: to 2^-36 of the row's largest at the
- * finest; bf16 with max_queries 1: as two parts, to 2^-15), rounded once to dtype; a query that sees nothing (ql > n), or whose scores are all
- * -infinity, gives zeros. Rows of q past the last query are neither read nor written.
+ * finest; bf16 with max_queries 1: as two parts, to 2^-15), rounded once to dtype; a query that
+ * sees nothing (ql > n), or whose scores are all -infinity, gives zeros. Rows of q past the last
+ * query are neither read nor written.
  * A query that sees a slot outside the pool gives NaN, no such slot is dereferenced. A request
  * whose slot range is malformed (negative start or count), which holds more than max_tokens slots
  * or more than max_queries queries gives NaN for its queries; one whose query range is

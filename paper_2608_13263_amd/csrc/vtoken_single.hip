@@ -786,7 +786,8 @@ void shared_kernel(PromptArgs a, int split_tokens, int splits) {
         sc[t][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[t][j], scale, -base));
         l += sc[t][j];
       }
-      const Weights x = weights_of<kBf16, kKind == 1>(sc[t][0], sc[t][1]), y = weights_of<kBf16, kKind == 1>(sc[t][2], sc[t][3]);
+      const Weights x = weights_of<kBf16, kKind == 1>(sc[t][0], sc[t][1]);
+      const Weights y = weights_of<kBf16, kKind == 1>(sc[t][2], sc[t][3]);
       w[t] = __builtin_bit_cast(i16x4, u32x2{x.hi, y.hi});
       w_lo[t] = __builtin_bit_cast(i16x4, u32x2{x.lo, y.lo});
     }
